@@ -198,6 +198,65 @@ gaconv_status_t gaconv_dw_from_host_async(int32_t method, const void *x_host, co
                                     void *x_dev, void *dy_dev, float *dw_dev,
                                     const gaconv_conv_desc_t *desc, uint64_t seed, void *stream);
 
+/* ---- activations in 8 bits ------------------------------------------------------------------------------------------------
+ * What a training step keeps of a layer's input until the backward pass is read there for the filter gradient (its other use, by the
+ * elementwise layer in front, needs less).  These calls keep it in one byte an element and a scale for every GACONV_ACT_GROUP neighbouring
+ * channels, and take the filter gradient from that.  (No counterpart in the paper, which approximates the other operand, dY.)
+ *
+ * Rows are tokens, or pixels of a channels-last activation; a row has cols channels.
+ *   codes   uint8 [rows][pitch],  pitch = cols rounded up to a multiple of 16 (the bytes behind the channels are written as 0)
+ *   scales  uint8 [rows][groups], groups = cols / GACONV_ACT_GROUP, rounded up; a byte b stands for 2^(b-127) (E8M0)
+ * A group's exponent e is the least for which its largest magnitude is at most M * 2^e (M = 448 for E4M3, 127 for INT8), held to
+ * [-117, 119] and [-117, 121]; a code is x * 2^-e rounded to nearest, ties to even, and held to [-M, M].  The value code * 2^e is exact in
+ * bf16.  A group with an Inf or NaN gets scale byte 255 and codes 0 and reads back as NaN throughout.  (E4M3 codes 0x7f and 0xff, which these
+ * calls never write, would read back as +-480.) */
+#define GACONV_ACT_GROUP 32
+typedef enum { GACONV_ACT_E4M3 = 0, GACONV_ACT_INT8 = 1 } gaconv_act_format_t;
+
+typedef struct gaconv_rows_desc {
+    uint32_t struct_size;              /* = sizeof(gaconv_rows_desc_t); versions the struct               */
+    int32_t  cols;                     /* channels of a row, at least 1                                   */
+    int64_t  rows;                     /* 0 to 2^31 - 1; 0: the call writes nothing (a weight gradient: zeros) */
+    int32_t  dtype;                    /* gaconv_dtype_t of the plain tensors                             */
+    int32_t  format;                   /* gaconv_act_format_t of codes                                    */
+    int64_t  x_stride, r_stride, s_stride, y_stride;   /* elements from a row to the next of x, residual, sum, y and of their gradients; 0: cols.
+                                          Multiples of 16 bytes are read fastest                          */
+    float    eps;                      /* norm: added to the mean square, at least 0                      */
+} gaconv_rows_desc_t;
+
+/* Bytes of codes and scales for desc->rows rows. */
+gaconv_status_t gaconv_act_sizes(const gaconv_rows_desc_t *desc, size_t *codes_bytes, size_t *scales_bytes);
+/* x [rows][cols], rows x_stride apart -> codes, scales. */
+gaconv_status_t gaconv_act_pack(const void *x, void *codes, void *scales, const gaconv_rows_desc_t *desc, void *stream);
+/* codes, scales -> x [rows][cols], rows x_stride apart (what lies between the rows is left as it is). */
+gaconv_status_t gaconv_act_unpack(const void *codes, const void *scales, void *x, const gaconv_rows_desc_t *desc, void *stream);
+
+/* gaconv_dw_exact (method GACONV_METHOD_EXACT) or gaconv_dw_approx (another method) with X as codes and scales of `format`: its rows are the
+ * n*h*w pixels, its channels the c channels, desc->x_layout is GACONV_X_NHWC (otherwise GACONV_ERR_UNSUPPORTED).  A linear layer on m tokens is
+ * n = m, h = w = r = s = 1.  desc->in_dtype is the type of dy.  desc->workspace: at least gaconv_packed_workspace_size bytes, prepared by
+ * gaconv_workspace_init.  ZERO and RANDOM read neither codes, scales, dy nor workspace; they may be NULL.
+ * Values that are not finite: as gaconv_dw_exact has them for kernels other than the channels-last one. */
+gaconv_status_t gaconv_dw_from_packed(int32_t method, const void *codes, const void *scales, int32_t format, const void *dy, float *dw,
+                                      const gaconv_conv_desc_t *desc, uint64_t seed, void *stream);
+gaconv_status_t gaconv_packed_workspace_size(const gaconv_conv_desc_t *desc, int32_t method, size_t *bytes);
+
+/* ---- root-mean-square norm of rows, with the residual's addition in front and the output in 8 bits beside it --------------------
+ *   sum = x + residual, rounded to dtype;  rstd = 1 / sqrt(mean over the row of sum^2 + eps);  y = sum * rstd * weight, rounded to dtype;
+ *   codes, scales = gaconv_act_pack(y).
+ * weight: cols elements of dtype; rstd: rows floats.  residual may be NULL (sum = x).  Outputs that may be NULL: sum where residual is, rstd,
+ * y where codes are given, and codes with scales.  sum may be the buffer of x or of residual (same stride); nothing else may overlap. */
+gaconv_status_t gaconv_rmsnorm_forward(const void *x, const void *residual, const void *weight, void *sum, void *y, void *codes, void *scales,
+                                       float *rstd, const gaconv_rows_desc_t *desc, void *stream);
+/* Its gradients: with h = sum * rstd and g = dy * weight
+ *   dx = dsum + rstd * (g - h * mean over the row of g h), rounded to dtype: the gradient of x, and of residual;
+ *   dweight = sum over rows of dy * h (fp32).
+ * dsum, the gradient that reaches sum from elsewhere, may be NULL (zero); dweight may be NULL (not wanted; no workspace then).  dx may be dsum's
+ * buffer (same stride); nothing else may overlap.  workspace: gaconv_rmsnorm_workspace_size bytes of device scratch, not initialised; calls that
+ * can overlap on the GPU need one each. */
+gaconv_status_t gaconv_rmsnorm_backward(const void *dy, const void *dsum, const void *sum, const void *weight, const float *rstd, void *dx,
+                                        float *dweight, const gaconv_rows_desc_t *desc, void *workspace, size_t workspace_bytes, void *stream);
+gaconv_status_t gaconv_rmsnorm_workspace_size(const gaconv_rows_desc_t *desc, size_t *bytes);
+
 /* Waits for `stream`, then reports GACONV_ERR_TIMEOUT if a kernel that used desc->workspace gave up
  * on a bounded wait since the last poll (and clears the flag), GACONV_OK otherwise. */
 gaconv_status_t gaconv_poll_async_status(const gaconv_conv_desc_t *desc, void *stream);

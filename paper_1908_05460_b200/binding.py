@@ -26,6 +26,8 @@ METHOD_EXACT, METHOD_ZERO, METHOD_RANDOM, METHOD_TOP1, METHOD_TOPK = -1, 0, 1, 2
 MAX_TOPK = 16
 MATH_DEFAULT, MATH_TF32 = 0, 1
 ALGO_AUTO, ALGO_DIRECT, ALGO_TENSOR = 0, 1, 2
+ACT_E4M3, ACT_INT8 = 0, 1
+ACT_GROUP = 32
 SCHED_EVERY_4TH_LAYER, SCHED_ALT_LAYER_ALT_BATCH, SCHED_ALL_LAYERS_EVERY_4TH_BATCH, SCHED_LAYER2_ALT_BATCH, \
     SCHED_SEEDED_FRACTION_ALT_BATCH = range(5)
 
@@ -33,6 +35,8 @@ EXPORTS = [
     "gaconv_status_string", "gaconv_launch_count", "gaconv_workspace_size", "gaconv_workspace_init", "gaconv_dw_exact",
     "gaconv_dw_approx", "gaconv_approx_select", "gaconv_dw_from_host", "gaconv_dw_from_host_async", "gaconv_poll_async_status",
     "gaconv_schedule_create", "gaconv_schedule_method", "gaconv_schedule_run_layer", "gaconv_schedule_run_step", "gaconv_schedule_destroy",
+    "gaconv_act_sizes", "gaconv_act_pack", "gaconv_act_unpack", "gaconv_dw_from_packed", "gaconv_packed_workspace_size",
+    "gaconv_rmsnorm_forward", "gaconv_rmsnorm_backward", "gaconv_rmsnorm_workspace_size",
     "gaconv_dw_exact_static", "gaconv_static_scratch_bytes", "gaconv_poll_async_status_static", "gaconv_approx_select_topk",
 ]
 
@@ -43,6 +47,12 @@ class ConvDesc(ctypes.Structure):
                                        "in_dtype", "x_layout", "dy_layout", "dw_layout", "math", "algo", "topk", "sm_budget")] + \
         [("alpha", ctypes.c_float), ("rand_std", ctypes.c_float),
          ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class RowsDesc(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("cols", ctypes.c_int32), ("rows", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("format", ctypes.c_int32)] + [(f, ctypes.c_int64) for f in ("x_stride", "r_stride", "s_stride", "y_stride")] + \
+        [("eps", ctypes.c_float)]
 
 
 class GaconvError(RuntimeError):
@@ -82,6 +92,15 @@ def load():
     lib.gaconv_poll_async_status.argtypes = [dp, vp]
     lib.gaconv_poll_async_status_static.argtypes = [vp]
     lib.gaconv_approx_select_topk.argtypes = [vp, vp, vp, dp, vp]
+    rp = ctypes.POINTER(RowsDesc)
+    lib.gaconv_act_sizes.argtypes = [rp, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    lib.gaconv_act_pack.argtypes = [vp, vp, vp, rp, vp]
+    lib.gaconv_act_unpack.argtypes = [vp, vp, vp, rp, vp]
+    lib.gaconv_dw_from_packed.argtypes = [i32, vp, vp, i32, vp, vp, dp, u64, vp]
+    lib.gaconv_packed_workspace_size.argtypes = [dp, i32, ctypes.POINTER(sz)]
+    lib.gaconv_rmsnorm_forward.argtypes = [vp] * 8 + [rp, vp]
+    lib.gaconv_rmsnorm_backward.argtypes = [vp] * 7 + [rp, vp, sz, vp]
+    lib.gaconv_rmsnorm_workspace_size.argtypes = [rp, ctypes.POINTER(sz)]
     lib.gaconv_schedule_create.argtypes = [ctypes.POINTER(vp), i32, i32, i32, ctypes.c_double, u64]
     lib.gaconv_schedule_method.argtypes = [vp, i32, ctypes.c_int64]
     lib.gaconv_schedule_method.restype = i32
@@ -204,6 +223,72 @@ def gaconv_dw_from_host_async(method: int, x_host, dy_host, dw_host, x_dev, dy_d
                               stream=None):
     _check(load().gaconv_dw_from_host_async(method, _ptr(x_host), _ptr(dy_host), _ptr(dw_host), _ptr(x_dev), _ptr(dy_dev),
                                             _ptr(dw_dev), ctypes.byref(desc), seed, _stream(stream)), "gaconv_dw_from_host_async")
+
+
+def make_rows_desc(rows: int, cols: int, dtype: torch.dtype, *, fmt=ACT_E4M3, eps=0.0, x_stride=0, r_stride=0, s_stride=0,
+                   y_stride=0) -> RowsDesc:
+    d = RowsDesc()
+    d.struct_size = ctypes.sizeof(RowsDesc)
+    d.rows, d.cols, d.format, d.eps = rows, cols, fmt, eps
+    d.dtype = BF16 if dtype == torch.bfloat16 else F32
+    d.x_stride, d.r_stride, d.s_stride, d.y_stride = x_stride, r_stride, s_stride, y_stride
+    return d
+
+
+def gaconv_act_sizes(desc: RowsDesc) -> tuple[int, int]:
+    codes, scales = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(load().gaconv_act_sizes(ctypes.byref(desc), ctypes.byref(codes), ctypes.byref(scales)), "gaconv_act_sizes")
+    return codes.value, scales.value
+
+
+def gaconv_act_pack(x, codes, scales, desc: RowsDesc, stream=None):
+    _check(load().gaconv_act_pack(_ptr(x), _ptr(codes), _ptr(scales), ctypes.byref(desc), _stream(stream)), "gaconv_act_pack")
+
+
+def gaconv_act_unpack(codes, scales, x, desc: RowsDesc, stream=None):
+    _check(load().gaconv_act_unpack(_ptr(codes), _ptr(scales), _ptr(x), ctypes.byref(desc), _stream(stream)), "gaconv_act_unpack")
+
+
+def gaconv_packed_workspace_size(desc: ConvDesc, method: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().gaconv_packed_workspace_size(ctypes.byref(desc), method, ctypes.byref(out)), "gaconv_packed_workspace_size")
+    return out.value
+
+
+def attach_packed_workspace(desc: ConvDesc, methods=(METHOD_EXACT,), device="cuda") -> torch.Tensor:
+    """attach_workspace for gaconv_dw_from_packed with `methods`."""
+    need = max(gaconv_packed_workspace_size(desc, m) for m in methods)
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    gaconv_workspace_init(ws, need)
+    desc.workspace, desc.workspace_bytes = ws.data_ptr(), need
+    return ws
+
+
+def gaconv_dw_from_packed(method: int, codes, scales, fmt: int, dy, dw, desc: ConvDesc, seed: int = 0, stream=None):
+    _check(load().gaconv_dw_from_packed(method, _ptr(codes), _ptr(scales), fmt, _ptr(dy), _ptr(dw), ctypes.byref(desc), seed,
+                                        _stream(stream)), "gaconv_dw_from_packed")
+
+
+def gaconv_rmsnorm_forward(x, residual, weight, sum_, y, codes, scales, rstd, desc: RowsDesc, stream=None):
+    _check(load().gaconv_rmsnorm_forward(_ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_), _ptr(y), _ptr(codes), _ptr(scales),
+                                         _ptr(rstd), ctypes.byref(desc), _stream(stream)), "gaconv_rmsnorm_forward")
+
+
+def gaconv_rmsnorm_workspace_size(desc: RowsDesc) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().gaconv_rmsnorm_workspace_size(ctypes.byref(desc), ctypes.byref(out)), "gaconv_rmsnorm_workspace_size")
+    return out.value
+
+
+def rmsnorm_workspace(desc: RowsDesc, device="cuda") -> torch.Tensor:
+    """Scratch for gaconv_rmsnorm_backward."""
+    return torch.empty(gaconv_rmsnorm_workspace_size(desc), dtype=torch.uint8, device=device)
+
+
+def gaconv_rmsnorm_backward(dy, dsum, sum_, weight, rstd, dx, dweight, desc: RowsDesc, workspace=None, stream=None):
+    _check(load().gaconv_rmsnorm_backward(_ptr(dy), _ptr(dsum), _ptr(sum_), _ptr(weight), _ptr(rstd), _ptr(dx), _ptr(dweight),
+                                          ctypes.byref(desc), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                          _stream(stream)), "gaconv_rmsnorm_backward")
 
 
 def gaconv_poll_async_status(desc: ConvDesc, stream=None) -> int:

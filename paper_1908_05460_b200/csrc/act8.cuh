@@ -1,0 +1,165 @@
+// Activations in 8 bits: groups of 32 neighbouring channels of a row share a power-of-two scale.  Device pieces shared by the kernels that
+// write and read them.
+//
+//   a = max |x| of the group,  e = least integer with a <= M 2^e (M = 448 for E4M3, 127 for INT8), held to [-117, 119] / [-117, 121]
+//   code = x 2^-e rounded to the 8-bit format (to nearest, ties to even; beyond +-M: +-M),  value = code 2^e,  scale byte = e + 127 (E8M0)
+//
+// A value has 4 (E4M3) or 7 (INT8) significant bits and, by the limits of e, is a finite and normal bf16 number or zero: reading back is exact,
+// and so is a product with a bf16 number on the tensor cores.  (At the upper limit elements beyond 448 2^119 and 127 2^121, above 2.9e38,
+// are held to it, since the next code times the scale would be infinite.)
+// A group with an element that is not finite has scale byte 255 and codes 0; all of it reads back as NaN.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+#include <stdint.h>
+
+#include "gaconv.h"
+
+namespace gaconv {
+
+constexpr int kActGroup = GACONV_ACT_GROUP;
+static_assert(kActGroup == 32, "lanes of four share a group of 32 channels");
+
+// scale byte of a group from the bits of its largest magnitude (fp32 bits without the sign; NaN counts as large)
+template <int FMT>
+__device__ __forceinline__ int act_scale_byte(uint32_t a)
+{
+    constexpr uint32_t top = FMT == GACONV_ACT_E4M3 ? 0x600000u : 0x7e0000u;       // fraction of M: 448 = 1.75 2^8, 127 = 1.984375 2^6
+    constexpr int bits = FMT == GACONV_ACT_E4M3 ? 8 : 6, hi = FMT == GACONV_ACT_E4M3 ? 119 : 121;
+    if (a >= 0x7f800000u) return 255;
+    const int e = (int)(a >> 23) - 127 - bits + ((a & 0x7fffffu) > top ? 1 : 0);      // (subnormal: below the limit whatever the fraction)
+    return min(max(e, -117), hi) + 127;
+}
+// 2^-e of a scale byte as a float (exact: a normal number), 0 for groups that are not finite
+__device__ __forceinline__ float act_inverse(int byte) { return byte == 255 ? 0.f : __uint_as_float((uint32_t)(254 - byte) << 23); }
+
+// four scaled values -> four codes.  A NaN (only where the scale is 0: Inf or NaN times 0) must be taken out by the caller.
+template <int FMT>
+__device__ __forceinline__ uint32_t act_encode4(float a, float b, float c, float d)
+{
+    if constexpr (FMT == GACONV_ACT_E4M3) {
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+        return lo | hi << 16;
+    } else {
+        auto q = [](float v) { return (uint32_t)__float2int_rn(fminf(fmaxf(v, -127.f), 127.f)) & 255u; };
+        return q(a) | q(b) << 8 | q(c) << 16 | q(d) << 24;
+    }
+}
+
+__device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t bf2_sub(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// 2^e of a scale byte, twice, as bf16
+__device__ __forceinline__ uint32_t act_scale2(uint32_t byte)
+{
+    const uint32_t s = byte == 255 ? 0x7fc0u : byte == 0 ? 0x40u : byte << 7;
+    return s | s << 16;
+}
+// four codes -> their values times 2^e, bf16 pairs.  E4M3: the code's exponent and fraction moved to their places in a bf16 number stand
+// for the value times 2^-120, subnormals included; the two products are exact.  (Codes 0x7f and 0xff, which nothing here writes, give 480.)
+// INT8: 128 + the low seven bits, less 128 or, with the sign bit, 256: bf16 numbers from 128 to 256 are whole and put together by bits.
+template <int FMT>
+__device__ __forceinline__ uint2 act_decode4(uint32_t w, uint32_t scale2)
+{
+    uint2 v;
+    if constexpr (FMT == GACONV_ACT_E4M3) {
+        const uint32_t lo = __byte_perm(w, 0, 0x1404), hi = __byte_perm(w, 0, 0x3424), up = 0x7b807b80u;       // 2^120
+        v.x = bf2_mul(lo >> 4 & 0x07f007f0u | lo & 0x80008000u, up);
+        v.y = bf2_mul(hi >> 4 & 0x07f007f0u | hi & 0x80008000u, up);
+    } else {
+        const uint32_t lo = __byte_perm(w, 0, 0x4140), hi = __byte_perm(w, 0, 0x4342), base = 0x43004300u;
+        v.x = bf2_sub(lo & 0x007f007fu | base, lo & 0x00800080u | base);
+        v.y = bf2_sub(hi & 0x007f007fu | base, hi & 0x00800080u | base);
+    }
+    v.x = bf2_mul(v.x, scale2);
+    v.y = bf2_mul(v.y, scale2);
+    return v;
+}
+
+// ---- eight neighbouring elements of a row as fp32 ----
+// VEC: the eight lie on a 16-byte boundary, otherwise they are read or written one by one; `left`: how many of them the row has
+template <bool VEC>
+__device__ __forceinline__ void load8(const float* p, int left, float (&v)[8])
+{
+    if (VEC && left >= 8) {
+        const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.f;
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, int left, float (&v)[8])
+{
+    if (VEC && left >= 8) {
+        const uint4 t = *reinterpret_cast<const uint4*>(p);
+        const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? __bfloat162float(p[i]) : 0.f;
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(float* p, int left, const float (&v)[8])
+{
+    if (VEC && left >= 8) {
+        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < left) p[i] = v[i];
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(__nv_bfloat16* p, int left, const float (&v)[8])
+{
+    if (VEC && left >= 8) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&t);
+        }
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < left) p[i] = __float2bfloat16_rn(v[i]);
+    }
+}
+// the value that an element of the type has
+__device__ __forceinline__ float rounded(float v, const float*) { return v; }
+__device__ __forceinline__ float rounded(float v, const __nv_bfloat16*) { return __bfloat162float(__float2bfloat16_rn(v)); }
+
+// Quantises eight elements; the four lanes of an aligned quartet hold the 32 channels of a group and call together (elements past the row: 0).
+// Writes the codes, and from the quartet's first lane the scale.  codes: the row's, at the eight; `pitch_left`: bytes of the row from there.
+template <int FMT>
+__device__ __forceinline__ void act_store8(const float (&v)[8], uint8_t* codes, int pitch_left, uint8_t* scale, bool first)
+{
+    uint32_t a = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(v[i]) & 0x7fffffffu);
+    a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
+    a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
+    if (pitch_left <= 0) return;
+    const int byte = act_scale_byte<FMT>(a);
+    const float inv = act_inverse(byte);
+    uint2 q = make_uint2(act_encode4<FMT>(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv), act_encode4<FMT>(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
+    if (byte == 255) q = make_uint2(0, 0);
+    *reinterpret_cast<uint2*>(codes) = q;
+    if (first) *scale = (uint8_t)byte;
+}
+
+}  // namespace gaconv

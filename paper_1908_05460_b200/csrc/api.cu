@@ -17,11 +17,7 @@ using namespace gaconv;
 static std::atomic<uint64_t> g_launches{0};
 void gaconv::note_launch(int count) { g_launches.fetch_add((uint64_t)count, std::memory_order_relaxed); }
 
-namespace {
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-gaconv_status_t make_geom(const gaconv_conv_desc_t* d, Geom* g)
+gaconv_status_t gaconv::make_geom(const gaconv_conv_desc_t* d, Geom* g)
 {
     if (d == nullptr) return GACONV_ERR_NULL_POINTER;
     if (d->struct_size != sizeof(gaconv_conv_desc_t)) return GACONV_ERR_BAD_DESC;
@@ -59,6 +55,8 @@ gaconv_status_t make_geom(const gaconv_conv_desc_t* d, Geom* g)
     g->sm_budget = d->sm_budget;
     return GACONV_OK;
 }
+
+namespace {
 
 // ---- plans are kept: the planners run once per (problem, device), not once per call --------------------------------
 // A key is every field a plan depends on, plus the device (SM count and resident clusters differ between devices).

@@ -201,8 +201,30 @@ bool plan_cl(const Geom& g, bool dy_npqk, size_t limit, ClPlan* plan);
 cudaError_t launch_cl(const void* x, const void* dy, float* dw, float* partial, void* x_scratch, void* dy_scratch, uint32_t* status,
                       const ClPlan& plan, bool wide, cudaStream_t stream);        // wide: the copies on aligned rows
 
+// ---- rows of activations in 8 bits (act8.cuh) ----
+struct ActRows { long long rows, stride; int cols, format; bool bf16; };       // of the plain tensor: stride in elements, type
+inline int act_pitch(int cols) { return (cols + 15) / 16 * 16; }               // bytes of a row of codes: rows start where a copy engine can
+inline int act_groups(int cols) { return (cols + GACONV_ACT_GROUP - 1) / GACONV_ACT_GROUP; }
+cudaError_t launch_act_pack(const void* x, void* codes, void* scales, const ActRows& a, cudaStream_t stream);
+cudaError_t launch_act_unpack(const void* codes, const void* scales, void* x, const ActRows& a, cudaStream_t stream);
+
+// ---- root-mean-square norm ----
+struct NormRows {
+    long long rows, x_stride, r_stride, s_stride, y_stride;
+    int cols, format, pitch, groups;
+    float eps;
+    bool bf16;
+};
+int norm_partials(const NormRows& o);
+cudaError_t launch_rmsnorm_forward(const NormRows& o, const void* x, const void* res, const void* w, void* sum, void* y, void* codes, void* scales, float* rstd, cudaStream_t stream);
+// partial: norm_partials() x cols floats (dweight == nullptr: unused)
+cudaError_t launch_rmsnorm_backward(const NormRows& o, const void* dy, const void* ds, const void* s, const void* w, const float* rstd, void* dx, float* dweight, float* partial, cudaStream_t stream);
+
 int device_sms();       // SMs of the current device
 bool tensor_maps_available();       // the driver's tensor-map encoder was found
+
+gaconv_status_t make_geom(const gaconv_conv_desc_t* d, Geom* g);       // validates
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // The scratch that a call given `given` bytes of it uses; more than `given`: the call is refused.  (kNoLimit: gaconv_workspace_size.)
 gaconv_status_t method_workspace(const gaconv_conv_desc_t* desc, int32_t method, size_t given, size_t* bytes);
