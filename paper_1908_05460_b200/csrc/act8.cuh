@@ -59,23 +59,20 @@ __device__ __forceinline__ uint32_t bf2_sub(uint32_t a, uint32_t b)
     asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
-// 2^e of a scale byte, twice, as bf16
-__device__ __forceinline__ uint32_t act_scale2(uint32_t byte)
-{
-    const uint32_t s = byte == 255 ? 0x7fc0u : byte == 0 ? 0x40u : byte << 7;
-    return s | s << 16;
-}
-// four codes -> their values times 2^e, bf16 pairs.  E4M3: the code's exponent and fraction moved to their places in a bf16 number stand
-// for the value times 2^-120, subnormals included; the two products are exact.  (Codes 0x7f and 0xff, which nothing here writes, give 480.)
-// INT8: 128 + the low seven bits, less 128 or, with the sign bit, 256: bf16 numbers from 128 to 256 are whole and put together by bits.
+// four codes -> their values times a power of two, bf16 pairs.  E4M3: the code's exponent and fraction moved to their places in a bf16 number stand
+// for the value times 2^-120, subnormals included, and `scale2` (from act_scale2) makes up for it; the product is exact.  (Codes 0x7f and 0xff,
+// which nothing here writes, give 480.)  INT8: 128 + the low seven bits, less 128 or, with the sign bit, 256: bf16 numbers from 128 to 256 are
+// whole and put together by bits.
 template <int FMT>
 __device__ __forceinline__ uint2 act_decode4(uint32_t w, uint32_t scale2)
 {
     uint2 v;
     if constexpr (FMT == GACONV_ACT_E4M3) {
-        const uint32_t lo = __byte_perm(w, 0, 0x1404), hi = __byte_perm(w, 0, 0x3424), up = 0x7b807b80u;       // 2^120
-        v.x = bf2_mul(lo >> 4 & 0x07f007f0u | lo & 0x80008000u, up);
-        v.y = bf2_mul(hi >> 4 & 0x07f007f0u | hi & 0x80008000u, up);
+        // (a byte's sign eight times above the byte: shifted by four the sign is in its place, and what is too much is masked)
+        asm("prmt.b32 %0, %1, 0, 0x9180;" : "=r"(v.x) : "r"(w));
+        asm("prmt.b32 %0, %1, 0, 0xb3a2;" : "=r"(v.y) : "r"(w));
+        v.x = v.x << 4 & 0x87f087f0u;
+        v.y = v.y << 4 & 0x87f087f0u;
     } else {
         const uint32_t lo = __byte_perm(w, 0, 0x4140), hi = __byte_perm(w, 0, 0x4342), base = 0x43004300u;
         v.x = bf2_sub(lo & 0x007f007fu | base, lo & 0x00800080u | base);
@@ -83,6 +80,28 @@ __device__ __forceinline__ uint2 act_decode4(uint32_t w, uint32_t scale2)
     }
     v.x = bf2_mul(v.x, scale2);
     v.y = bf2_mul(v.y, scale2);
+    return v;
+}
+// The scale of a byte for act_decode4, twice, as bf16: 2^e for INT8, 2^(120 + e) for E4M3, of which bf16 has room for e up to 7; act_rest2 is
+// what is left of larger ones, another factor.  Byte 255: codes are 0, and 0 times infinity, or times the rest NaN, is NaN.
+template <int FMT>
+__device__ __forceinline__ uint32_t act_scale2(uint32_t byte)
+{
+    return FMT == GACONV_ACT_E4M3 ? min(byte, 134u) * 0x00800080u + 0x3c003c00u : byte * 0x00800080u;
+}
+template <int FMT> __device__ __forceinline__ bool act_has_rest(uint32_t byte) { return FMT == GACONV_ACT_E4M3 && byte > 134; }
+__device__ __forceinline__ uint32_t act_rest2(uint32_t byte) { return byte == 255 ? 0x7fc07fc0u : byte > 134 ? (byte - 134 + 127) * 0x00800080u : 0x3f803f80u; }
+// eight codes
+template <int FMT>
+__device__ __forceinline__ uint4 act_decode8(uint2 q, uint32_t byte)
+{
+    const uint32_t s2 = act_scale2<FMT>(byte);
+    const uint2 a = act_decode4<FMT>(q.x, s2), b = act_decode4<FMT>(q.y, s2);
+    uint4 v = make_uint4(a.x, a.y, b.x, b.y);
+    if (act_has_rest<FMT>(byte)) {
+        const uint32_t r = act_rest2(byte);
+        v = make_uint4(bf2_mul(v.x, r), bf2_mul(v.y, r), bf2_mul(v.z, r), bf2_mul(v.w, r));
+    }
     return v;
 }
 

@@ -71,9 +71,8 @@ act_unpack_kernel(const uint8_t* codes, const uint8_t* scales, T* x, const RowsO
         for (int i = 0; i < 4; ++i) {
             const int u = u0 + i * lanes;
             if (u >= units) break;
-            const uint32_t s2 = act_scale2(s[i]);
-            const uint2 a = act_decode4<FMT>(q[i].x, s2), b = act_decode4<FMT>(q[i].y, s2);
-            const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+            const uint4 d = act_decode8<FMT>(q[i], s[i]);
+            const uint32_t w[4] = {d.x, d.y, d.z, d.w};
             float v[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) { v[2 * j] = __uint_as_float(w[j] << 16); v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }

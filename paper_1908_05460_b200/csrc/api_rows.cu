@@ -34,14 +34,17 @@ NormRows norm_rows(const gaconv_rows_desc_t& d)
 }
 size_t norm_workspace(const NormRows& o) { return std::max<size_t>(256, align_up(sizeof(float) * (size_t)norm_partials(o) * o.cols, 256)); }
 
-// Scratch of a filter gradient from the 8-bit form: what the call on a plain X takes, and X itself behind it
-struct PackedLayout { size_t inner, total; bool reads; };
+// Scratch of a filter gradient from the 8-bit form: the sums of the kernel for linear layers, or what the call on a plain X takes and X itself behind it
+struct PackedLayout { size_t inner, total; bool reads, fused; PackedPlan plan; };
 gaconv_status_t packed_layout(const gaconv_conv_desc_t* desc, int32_t method, Geom* g, PackedLayout* L)
 {
     gaconv_status_t st = make_geom(desc, g);
     if (st != GACONV_OK) return st;
     if (desc->x_layout != GACONV_X_NHWC || (long long)g->n * g->h > 0x7fffffffll / g->w || g->c > (1 << 30)) return GACONV_ERR_UNSUPPORTED;
     L->reads = method != GACONV_METHOD_ZERO && method != GACONV_METHOD_RANDOM;
+    // (ALGO_DIRECT and the one-pass TF32 mode name kernels of the plain form)
+    L->fused = method == GACONV_METHOD_EXACT && desc->algo != GACONV_ALGO_DIRECT && desc->math == GACONV_MATH_DEFAULT && plan_packed(*g, desc->dy_layout == GACONV_DY_NPQK, &L->plan);
+    if (L->fused) { L->inner = 0; L->total = align_up(kWsDataOffset, 256) + L->plan.partial_bytes + L->plan.dy_bytes; return GACONV_OK; }
     if ((st = method_workspace(desc, method, kNoLimit, &L->inner)) != GACONV_OK) return st;
     L->inner = align_up(L->inner, 256);
     L->total = L->inner + (L->reads ? align_up((size_t)g->n * g->h * g->w * g->c * (g->bf16 ? 2 : 4), 256) : 0);
@@ -109,6 +112,11 @@ gaconv_status_t gaconv_dw_from_packed(int32_t method, const void* codes, const v
     if (desc->math == GACONV_MATH_TF32 && g.bf16) return GACONV_ERR_BAD_DESC;
     if (desc->workspace_bytes < L.total) return GACONV_ERR_WORKSPACE_TOO_SMALL;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    if (L.fused) {
+        char *ws = static_cast<char*>(desc->workspace), *partial = ws + align_up(kWsDataOffset, 256);
+        return launch_packed(codes, scales, format, dy, dw, reinterpret_cast<float*>(partial), partial + L.plan.partial_bytes, reinterpret_cast<uint32_t*>(ws), g, L.plan, cs) == cudaSuccess
+                   ? GACONV_OK : GACONV_ERR_CUDA;
+    }
     gaconv_conv_desc_t inner = *desc;
     inner.workspace_bytes = L.inner;
     void* x = static_cast<char*>(desc->workspace) + L.inner;

@@ -1396,6 +1396,14 @@ bool plan_cl(const Geom& g, bool dy_npqk, size_t limit, ClPlan* out)
     return true;
 }
 
+cudaError_t launch_pack_rows(const void* src, void* dst, int ch, int pitch, int px, int n, bool channels_last, bool f32, cudaStream_t stream)
+{
+    const PackOp none{}, op = pack_op(src, dst, ch, pitch, px, n, channels_last, f32 ? kPackPx<float> : kPackPx<unsigned short>);
+    const cudaError_t err = launch_kernel(f32 ? pack_kernel<float, false> : pack_kernel<unsigned short, false>, dim3((unsigned)op.blocks), dim3(256), 0, stream, dim3(1, 1, 1), op, none);
+    if (err == cudaSuccess) note_launch();
+    return err;
+}
+
 cudaError_t launch_cl(const void* x, const void* dy, float* dw, float* partial, void* x_scratch, void* dy_scratch, uint32_t* status,
                       const ClPlan& plan, bool wide, cudaStream_t stream)
 {

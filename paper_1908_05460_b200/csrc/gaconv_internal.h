@@ -208,6 +208,15 @@ inline int act_groups(int cols) { return (cols + GACONV_ACT_GROUP - 1) / GACONV_
 cudaError_t launch_act_pack(const void* x, void* codes, void* scales, const ActRows& a, cudaStream_t stream);
 cudaError_t launch_act_unpack(const void* codes, const void* scales, void* x, const ActRows& a, cudaStream_t stream);
 
+// ---- filter gradient of a linear layer from X in 8 bits, on tcgen05 ----
+struct PackedPlan {
+    size_t partial_bytes, dy_bytes;         // workspace: sums of split tiles, packed copy of dY
+    alignas(8) unsigned char opaque[64];    // private to packed_dw.cu
+};
+bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan);       // false: not such a layer, or a gradient in another order
+cudaError_t launch_packed(const void* codes, const void* scales, int format, const void* dy, float* dw, float* partial, void* dy_scratch, uint32_t* status,
+                          const Geom& g, const PackedPlan& plan, cudaStream_t stream);
+
 // ---- root-mean-square norm ----
 struct NormRows {
     long long rows, x_stride, r_stride, s_stride, y_stride;
@@ -219,6 +228,9 @@ int norm_partials(const NormRows& o);
 cudaError_t launch_rmsnorm_forward(const NormRows& o, const void* x, const void* res, const void* w, void* sum, void* y, void* codes, void* scales, float* rstd, cudaStream_t stream);
 // partial: norm_partials() x cols floats (dweight == nullptr: unused)
 cudaError_t launch_rmsnorm_backward(const NormRows& o, const void* dy, const void* ds, const void* s, const void* w, const float* rstd, void* dx, float* dweight, float* partial, cudaStream_t stream);
+
+// n images of px pixels and ch channels, in either order -> rows of `pitch` (a multiple of 8) bf16 channels, zeros behind the ch; fp32: three such planes
+cudaError_t launch_pack_rows(const void* src, void* dst, int ch, int pitch, int px, int n, bool channels_last, bool f32, cudaStream_t stream);
 
 int device_sms();       // SMs of the current device
 bool tensor_maps_available();       // the driver's tensor-map encoder was found

@@ -1,0 +1,599 @@
+// Filter gradient of a linear layer (a 1x1 filter at stride 1) with X in 8 bits, on tcgen05:
+//
+//   dW[k, c] = alpha * sum over rows t of dY[t, k] * code[t, c] * 2^e[t, c / 32]
+//
+// The scales belong to the reduction index, so they cannot be taken out of the sum; but a code times its scale is exact in bf16 (act8.cuh).
+// So X goes from memory to the SM in 8 bits, is turned into bf16 on the way from one piece of shared memory to another, and lies there in the
+// order that the tensor core reads: half the bytes of a bf16 X and no copy of it in memory.  dY is the M side, X the N side, both MN-major (a row of
+// shared memory is a row t, 64 channels of it); fp32 gradients are three bf16 planes dY = d0 + d1 + d2 (8 + 8 + 8 bits) whose products add up
+// in the same accumulators.  Gradients that the copy engine cannot read as they lie (fp32, another order, a number of outputs that is no
+// multiple of 8) are packed into the workspace first.
+//
+// A CTA pair (CG = 2) shares a tile of 256 x 256: each CTA holds 128 outputs of dY and 128 channels of X, and the pair's MMAs read both halves of X,
+// so that a turned element serves 256 outputs.  (Shared memory is the bound: for 64 rows a CTA's MMAs read 32 KB, the copies write 16 + 8, and
+// turning reads 8 and writes 16, 80 KB at 128 bytes a cycle beside the 512 cycles of the MMAs; with tiles of 128 x 128 it is as much beside 256.)
+// CG = 1: tiles of 128 x 128 for problems that would not fill the GPU with larger ones.
+//
+// Whoever turns X loads nothing from memory: the fence between its stores and the tensor core waits for every load that the thread has in flight
+// (loads two stages ahead in its registers: 1435 us for 16384 rows, 4096 -> 4096, where the wait alone was three times the MMAs).
+//
+// The tensor core adds by truncation, so accumulators are handed over every `epoch` stages to eight warps that add them up in fp32 registers; two
+// accumulator sets alternate.  CTAs stay and take units (a tile, a range of rows) in turn; pipeline and sets run on from unit to unit, so
+// that the writing of one hides behind the next.  The tiles of a last, incomplete round are split over their rows; the splits meet in the workspace,
+// added in order by packed_reduce_kernel.
+//
+// Rows past the end and channels past a row are zeros on both sides.  Every wait is bounded; on expiry the kernel raises the workspace status word,
+// lets its copies and MMAs land, frees its tensor memory and returns.
+#include <cuda.h>
+
+#include <algorithm>
+#include <cstring>
+
+#include "act8.cuh"
+#include "gaconv_internal.h"
+#include "tma.cuh"
+#include "umma.cuh"
+
+namespace gaconv {
+namespace {
+
+constexpr int kRows = 64;                           // rows t of a stage
+constexpr int kTile = kRows * 128;                  // bytes of 64 channels of a stage
+constexpr int kRaw = kRows * 128 + kRows * 8;       // 128 channels in 8 bits, and the two words around the four scales of each row
+constexpr int kThreads = 640;                       // warps 0-3: copies of dY, MMAs, copies of X and scales, scales; 4-11 turn X, 12-19 sum
+constexpr int kMaxDy = 6, kMaxRaw = 7, kTurned = 3;    // stages of dY, of X in 8 bits, of X turned
+
+template <int CG, int PLANES> struct Config {
+    static constexpr int cols = 128 * CG, dy_stage = 2 * PLANES * kTile, dys = PLANES == 3 ? 3 : 6, raws = PLANES == 3 ? 3 : 7;
+    static constexpr int turned_at = dys * dy_stage, raw_at = turned_at + kTurned * 2 * kTile, bytes = raw_at + raws * kRaw;
+    static constexpr int epoch = PLANES == 3 ? 4 : 16;             // stages: chains of 48 or 64 MMAs
+    // registers of a thread by role; their sum over the warps is within what the block is launched with (96 each)
+    static constexpr int regs_control = 40, regs_turn = CG == 2 ? 56 : 80, regs_sum = CG == 2 ? 160 : 104;
+    static_assert(4 * regs_control + 8 * regs_turn + 8 * regs_sum <= 20 * 96, "registers");
+    static_assert(dys <= kMaxDy && raws <= kMaxRaw && bytes <= 225 * 1024, "shared memory");
+};
+
+struct PackedParams {
+    const uint8_t *codes, *scales;
+    float *dw, *partial;
+    uint32_t* status;
+    int rows, c, k, groups;
+    long long ws_k, ws_c;
+    float alpha;
+    int tiles_c;                                    // tile = tk * tiles_c + tc
+    int full, splits, units;                        // tiles [0, full) are units of their own; the others `splits` each
+    int chunks;                                     // stages of all rows
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+// wait for arrivals of either CTA of a pair
+__device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity)
+{
+    for (uint32_t i = 0; i < kWaitLimit; ++i) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+    }
+    return false;
+}
+template <int CG>
+__device__ __forceinline__ void arrive_leader(uint32_t bar)
+{
+    if (CG == 2) {
+        asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\tmbarrier.arrive.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
+    } else {
+        asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+    }
+}
+template <int CG>
+__device__ __forceinline__ void commit(uint32_t bar)       // to the barrier in every CTA of the group
+{
+    if (CG == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+    else umma_commit(bar);
+}
+template <int CG>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    if (CG == 2)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
+    else umma_bf16(d, a, b, idesc, accumulate);
+}
+template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+__device__ __forceinline__ void store_shared16(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ uint4 load_shared16(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+// asynchronous copy of a word, of which only the first n bytes are read; zeros behind them
+__device__ __forceinline__ void copy_word(uint32_t dst, const void* src, int n)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+// The stages of a CTA, unit after unit
+struct Walk {
+    int unit, left, chunk, k0, c0;
+    __device__ __forceinline__ void enter(const PackedParams& P)
+    {
+        left = 0;
+        if (unit >= P.units) return;
+        int tile = unit, first = 0, last = P.chunks;
+        if (unit >= P.full) {
+            const int u = unit - P.full, t = u / P.splits, s = u - t * P.splits;
+            tile = P.full + t;
+            first = (int)((long long)P.chunks * s / P.splits);
+            last = (int)((long long)P.chunks * (s + 1) / P.splits);
+        }
+        const int tk = tile / P.tiles_c;
+        k0 = tk; c0 = tile - tk * P.tiles_c;
+        chunk = first; left = last - first;
+    }
+    __device__ __forceinline__ void start(const PackedParams& P, int first_unit) { unit = first_unit; enter(P); }
+    __device__ __forceinline__ bool live() const { return left > 0; }
+    __device__ __forceinline__ void next(const PackedParams& P, int step)
+    {
+        ++chunk;
+        if (--left == 0) { unit += step; enter(P); }
+    }
+};
+
+template <int CG, int PLANES, int FMT>
+__global__ void __launch_bounds__(kThreads, 1)
+packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ PackedParams P)
+{
+    typedef Config<CG, PLANES> C;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bar_full[kTurned], bar_read[kTurned], bar_dy[kMaxDy], bar_free_dy[kMaxDy], bar_raw[kMaxRaw], bar_taken[kMaxRaw], bar_acc[2], bar_free[2], bar_last;
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile int s_abort;
+
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = CG == 2 ? (int)cluster_rank() : 0, group = blockIdx.x / CG, step = gridDim.x / CG;
+
+    pdl_release_next_grid();
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kTurned; ++i) { mbar_init(smem_u32(&bar_full[i]), 4 * CG + CG - 1); mbar_init(smem_u32(&bar_read[i]), 1); }
+        for (int i = 0; i < C::dys; ++i) { mbar_init(smem_u32(&bar_dy[i]), 1); mbar_init(smem_u32(&bar_free_dy[i]), 1); }
+        for (int i = 0; i < C::raws; ++i) { mbar_init(smem_u32(&bar_raw[i]), 1 + 64); mbar_init(smem_u32(&bar_taken[i]), 4); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bar_acc[i]), 1); mbar_init(smem_u32(&bar_free[i]), 8 * CG); }
+        mbar_init(smem_u32(&bar_last), 1);
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_dy) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
+    }
+    if (warp == 1) {
+        if (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(2 * C::cols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(2 * C::cols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (CG == 2) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = s_tmem;
+    pdl_wait_prior_grid();
+    auto give_up = [&] { s_abort = 1; atomicOr(P.status, 1u); };
+
+    if (warp < 4) {
+        regs_down<C::regs_control>();
+        if (warp == 0) {
+            // ------------------------------------------------------------ copies of dY: 64 rows x 128 outputs a stage and plane
+            Walk w;
+            w.start(P, group);
+            int st = 0, ph = 0, n = 0;
+            for (; w.live(); w.next(P, step), ++n) {
+                if (n >= C::dys && !pair_wait(smem_u32(&bar_free_dy[st]), ph ^ 1)) give_up();
+                if (__any_sync(0xffffffffu, s_abort)) break;
+                if (elect_one()) {
+                    const uint32_t bar = smem_u32(&bar_dy[st]), dst = base + st * C::dy_stage;
+                    mbar_expect_tx(bar, 2 * PLANES * kTile);
+                    const int k = (w.k0 * CG + rank) * 128, t = w.chunk * kRows;
+#pragma unroll
+                    for (int pl = 0; pl < PLANES; ++pl) {
+                        tma_load_3d(dst + 2 * pl * kTile, &map_dy, bar, k, t, pl);
+                        tma_load_3d(dst + (2 * pl + 1) * kTile, &map_dy, bar, k + 64, t, pl);
+                    }
+                }
+                __syncwarp();
+                if (++st == C::dys) { st = 0; ph ^= 1; }
+            }
+            // on failure the copies that were issued land; otherwise the last commits, which may come from the other CTA, arrive before this one goes (bounded)
+            const bool failed = __any_sync(0xffffffffu, s_abort);
+            for (int i = max(0, n - C::dys); i < n; ++i) pair_wait(smem_u32(failed ? &bar_dy[i % C::dys] : &bar_free_dy[i % C::dys]), (i / C::dys) & 1);
+        } else if (warp >= 2) {
+            // ------------------------------------------------------------ X in 8 bits: copies (warp 2), and scales, a row a lane of both warps
+            Walk w;
+            w.start(P, group);
+            int st = 0, ph = 0, n = 0;
+            bool ok = true;
+            const uint8_t* end = P.scales + (long long)P.rows * P.groups;
+            for (; w.live(); w.next(P, step), ++n) {
+                if (n >= C::raws && !mbar_wait(smem_u32(&bar_taken[st]), ph ^ 1)) give_up();
+                if (__any_sync(0xffffffffu, s_abort)) { ok = false; break; }
+                const uint32_t bar = smem_u32(&bar_raw[st]), dst = base + C::raw_at + st * kRaw;
+                if (warp == 2 && elect_one()) {
+                    mbar_expect_tx(bar, kRows * 128);
+                    tma_load_3d(dst, &map_x, bar, (w.c0 * CG + rank) * 128, w.chunk * kRows, 0);
+                }
+                __syncwarp();
+                // the row's scales lie on any byte: the one or two aligned words that hold them, no byte past the end
+                const int r = 32 * (warp - 2) + lane, row = w.chunk * kRows + r, g = (w.c0 * CG + rank) * 4;
+                const bool in = row < P.rows && g < P.groups;
+                const uint8_t* at = P.scales + (in ? (long long)row * P.groups + g : 0);
+                const int off = (int)(reinterpret_cast<uintptr_t>(at) & 3);
+                const ptrdiff_t left = end - (at - off);
+                const int n0 = in ? (int)min((ptrdiff_t)4, left) : 0, n1 = in && off != 0 ? (int)max((ptrdiff_t)0, min((ptrdiff_t)4, left - 4)) : 0;
+                copy_word(dst + kRows * 128 + r * 8, at - off, n0);
+                copy_word(dst + kRows * 128 + r * 8 + 4, n1 > 0 ? at - off + 4 : P.scales, n1);
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+                if (++st == C::raws) { st = 0; ph ^= 1; }
+            }
+            if (!ok) asm volatile("cp.async.wait_all;" ::: "memory");
+            if (!ok && warp == 2)        // the copies that were issued land (bounded; the other warp's share of the last barrier may be missing)
+                for (int i = max(0, n - C::raws); i < n; ++i) mbar_wait(smem_u32(&bar_raw[i % C::raws]), (i / C::raws) & 1);
+        } else if (CG == 2 && warp == 1 && rank == 1) {
+            // ------------------------------------------------------------ tells the leader of this CTA's copies of dY
+            Walk w;
+            w.start(P, group);
+            int st = 0, ds = 0, dph = 0;
+            for (; w.live(); w.next(P, step)) {
+                if (!mbar_wait(smem_u32(&bar_dy[ds]), dph)) give_up();
+                if (__any_sync(0xffffffffu, s_abort)) break;
+                if (lane == 0) arrive_leader<CG>(smem_u32(&bar_full[st]));
+                if (++st == kTurned) st = 0;
+                if (++ds == C::dys) { ds = 0; dph ^= 1; }
+            }
+        } else if (warp == 1 && rank == 0) {
+            // ------------------------------------------------------------ MMAs
+            // M = 128 a CTA, N = cols; bf16 operands, both MN-major, fp32 accumulators
+            constexpr uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(C::cols / 8) << 17 | (uint32_t)(8 * CG) << 24;
+            constexpr uint64_t hi = (uint64_t)(1024 / 16 | 1u << 14 | 2u << 29) << 32;          // eight rows to the next, 128-byte swizzle
+            constexpr uint32_t lbo = (uint32_t)(kTile / 16) << 16;                              // 64 channels to the next
+            Walk w;
+            w.start(P, group);
+            int st = 0, ph = 0, ds = 0, dph = 0, set = 0, in_epoch = 0, epochs = 0;
+            while (w.live()) {
+                if (in_epoch == 0 && epochs >= 2 && !pair_wait(smem_u32(&bar_free[set]), ((epochs >> 1) - 1) & 1)) give_up();
+                if (!s_abort && !(mbar_wait(smem_u32(&bar_dy[ds]), dph) && pair_wait(smem_u32(&bar_full[st]), ph))) give_up();
+                if (__any_sync(0xffffffffu, s_abort)) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const bool ends = w.left == 1 || in_epoch + 1 == C::epoch;
+                if (elect_one()) {
+                    const uint32_t a0 = base + ds * C::dy_stage, b0 = base + C::turned_at + st * 2 * kTile;
+                    const uint64_t a = hi | (lbo | (a0 >> 4)), b = hi | (lbo | (b0 >> 4));
+                    const uint32_t d = tmem + set * C::cols;
+#pragma unroll
+                    for (int i = 0; i < kRows / 16; ++i)
+#pragma unroll
+                        for (int pl = PLANES - 1; pl >= 0; --pl)
+                            mma<CG>(d, a + (pl * 2 * kTile + i * 2048) / 16, b + i * 2048 / 16, idesc, in_epoch > 0 || i > 0 || pl < PLANES - 1 ? 1u : 0u);
+                    commit<CG>(smem_u32(&bar_read[st]));
+                    commit<CG>(smem_u32(&bar_free_dy[ds]));
+                    if (ends) commit<CG>(smem_u32(&bar_acc[set]));
+                }
+                __syncwarp();
+                ++in_epoch;
+                if (ends) { in_epoch = 0; set ^= 1; ++epochs; }
+                if (++st == kTurned) { st = 0; ph ^= 1; }
+                if (++ds == C::dys) { ds = 0; dph ^= 1; }
+                w.next(P, step);
+            }
+            if (__any_sync(0xffffffffu, s_abort)) {      // the MMAs that were issued end (bounded)
+                if (elect_one()) {
+                    if (CG == 2) asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&bar_last)) : "memory");
+                    else umma_commit(smem_u32(&bar_last));
+                }
+                __syncwarp();
+                mbar_wait(smem_u32(&bar_last), 0);
+            }
+        }
+    } else if (warp < 12) {
+        // ---------------------------------------------------------------- X: 8 bits -> bf16
+        // Four warps take a stage, the other four the next.  A thread turns pieces of 16 channels, chunk q of rows `row` + 16 i.  Eight lanes take the
+        // lower 64 channels of a row and the upper 64 of its neighbour: then neither their reads nor their writes, whose chunks are permuted by
+        // the row, meet in a bank.
+        regs_down<C::regs_turn>();
+        const int t = threadIdx.x & 127, mine = (warp - 4) >> 2, q = t & 7, row = (t >> 3) ^ (q >> 2);
+        const uint32_t from = base + C::raw_at + row * 128 + 16 * q;
+        // (a row's first scale lies at byte (row * groups) % 4 of its two words, the same for rows 4 apart)
+        const uint32_t scale = base + C::raw_at + kRows * 128 + row * 8 + (row * P.groups & 3) + (q >> 1);
+        const uint32_t to = base + C::turned_at + (q >> 2) * kTile + row * 128, x0 = ((2 * (q & 3)) ^ (row & 7)) << 4;
+        Walk w;
+        w.start(P, group);
+        if (mine == 1 && w.live()) w.next(P, step);
+        int st = mine, ph = 0, rs = mine, rph = 0, n = mine;
+        bool ok = true;
+        while (w.live()) {
+            if (!mbar_wait(smem_u32(&bar_raw[rs]), rph)) give_up();
+            uint4 v[4];
+            uint32_t s[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = load_shared16(from + rs * kRaw + i * 2048);
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(s[i]) : "r"(scale + rs * kRaw + i * 128) : "memory");
+            }
+            if (n >= kTurned && !pair_wait(smem_u32(&bar_read[st]), ph ^ 1)) give_up();
+            if (__any_sync(0xffffffffu, s_abort)) { ok = false; break; }
+            const uint32_t dst = to + st * 2 * kTile;
+            const bool rest = __any_sync(0xffffffffu, act_has_rest<FMT>(max(max(s[0], s[1]), max(s[2], s[3]))));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t s2 = act_scale2<FMT>(s[i]);
+                uint2 d[4] = {act_decode4<FMT>(v[i].x, s2), act_decode4<FMT>(v[i].y, s2), act_decode4<FMT>(v[i].z, s2), act_decode4<FMT>(v[i].w, s2)};
+                if (rest) {
+                    const uint32_t r = act_rest2(s[i]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) d[j] = make_uint2(bf2_mul(d[j].x, r), bf2_mul(d[j].y, r));
+                }
+                store_shared16(dst + i * 2048 + x0, d[0].x, d[0].y, d[1].x, d[1].y);
+                store_shared16(dst + i * 2048 + (x0 ^ 16), d[2].x, d[2].y, d[3].x, d[3].y);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) { arrive_leader<CG>(smem_u32(&bar_full[st])); arrive(smem_u32(&bar_taken[rs])); }
+            for (st += 2; st >= kTurned; st -= kTurned) ph ^= 1;
+            for (rs += 2; rs >= C::raws; rs -= C::raws) rph ^= 1;
+            n += 2;
+            w.next(P, step);
+            if (w.live()) w.next(P, step);
+        }
+        // the last commits have arrived before this CTA goes (bounded; they may come from the other one)
+        if (ok && (warp & 3) == 0)
+            for (int i = n - 2; i >= 0 && i + kTurned >= n; i -= 2) pair_wait(smem_u32(&bar_read[i % kTurned]), (i / kTurned) & 1);
+    } else {
+        // ---------------------------------------------------------------- sums
+        // Warps w and w + 4 share 32 lanes of tensor memory (outputs) and take half of the columns (channels) each.
+        regs_up<C::regs_sum>();
+        constexpr int H = C::cols / 2;
+        const int sp = warp & 3, half = (warp - 12) >> 2, row = 32 * sp + lane;
+        float sum[H];
+        Walk w;
+        w.start(P, group);
+        int epochs = 0;
+        bool ok = true;
+        while (ok && w.live()) {
+            int left = w.left;
+            const int unit = w.unit, k = (w.k0 * CG + rank) * 128 + row, c0 = w.c0 * C::cols + half * H;
+            bool fresh = true;
+            for (; left > 0; left -= C::epoch) {
+                const int set = epochs & 1;
+                ok = pair_wait(smem_u32(&bar_acc[set]), (epochs >> 1) & 1);
+                if (!ok) give_up();
+                ok = __all_sync(0xffffffffu, ok && !s_abort);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (!ok) break;
+                const uint32_t src = tmem + set * C::cols + half * H + ((uint32_t)(32 * sp) << 16);
+                if (fresh) {
+#pragma unroll
+                    for (int i = 0; i < H; ++i) sum[i] = 0.f;
+                    fresh = false;
+                }
+#pragma unroll
+                for (int i = 0; i < H; i += 16) {
+                    float v[16];
+                    tmem_ld16_nowait(src + i, v);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum[i + e] += v[e];
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) arrive_leader<CG>(smem_u32(&bar_free[set]));
+                ++epochs;
+            }
+            if (!ok) break;
+            const bool whole = unit < P.full || P.splits == 1;
+            if (k < P.k) {
+                if (!whole) {
+                    // [tail unit][output][channel]
+                    float* out = P.partial + ((size_t)(unit - P.full) * (128 * CG) + rank * 128 + row) * C::cols + half * H;
+#pragma unroll
+                    for (int i = 0; i < H; i += 8)
+                        if (c0 + i < P.c)
+                            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + i), "f"(sum[i]), "f"(sum[i + 1]), "f"(sum[i + 2]),
+                                         "f"(sum[i + 3]), "f"(sum[i + 4]), "f"(sum[i + 5]), "f"(sum[i + 6]), "f"(sum[i + 7]) : "memory");
+                } else {
+                    float* out = P.dw + k * P.ws_k + c0 * P.ws_c;
+                    const float a = P.alpha;
+                    const bool sectors = P.ws_c == 1 && (P.ws_k & 7) == 0 && (reinterpret_cast<uintptr_t>(P.dw) & 31) == 0;
+#pragma unroll
+                    for (int i = 0; i < H; i += 8) {
+                        if (sectors && c0 + i + 8 <= P.c) {
+                            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + i), "f"(a * sum[i]), "f"(a * sum[i + 1]), "f"(a * sum[i + 2]),
+                                         "f"(a * sum[i + 3]), "f"(a * sum[i + 4]), "f"(a * sum[i + 5]), "f"(a * sum[i + 6]), "f"(a * sum[i + 7]) : "memory");
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (c0 + i + e < P.c) out[(i + e) * P.ws_c] = a * sum[i + e];
+                        }
+                    }
+                }
+            }
+            w.unit += step;
+            w.enter(P);
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (CG == 2) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * C::cols) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * C::cols) : "memory");
+    }
+}
+
+// dW of the split tiles: the sum of their splits in order.  Blocks of 256 threads: 1 << log_g groups of threads take splits g, g + G, ... of
+// 256 >> log_g quads of channels; the groups' sums meet in shared memory.  grid (quads / block, tail tiles)
+struct PackedReduce {
+    const float* partial;
+    float* dw;
+    long long ws_k, ws_c;
+    float alpha;
+    int c, k, side, tiles_c, full, splits, log_g;
+};
+__global__ void __launch_bounds__(256)
+packed_reduce_kernel(const __grid_constant__ PackedReduce R)
+{
+    __shared__ float4 s_sum[256];
+    pdl_release_next_grid();
+    const int G = 1 << R.log_g, per = 256 >> R.log_g, pos = threadIdx.x & (per - 1), g = threadIdx.x / per;
+    const int tile = R.full + blockIdx.y, tk = tile / R.tiles_c, tc = tile - tk * R.tiles_c;
+    const int quads = R.side >> 2, p = blockIdx.x * per + pos, row = p / quads, q = p - row * quads;
+    const int k = tk * R.side + row, c = tc * R.side + 4 * q;
+    const bool in = k < R.k && c < R.c;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    pdl_wait_prior_grid();
+    if (in) {
+        const size_t block = (size_t)R.side * R.side;
+        const float* src = R.partial + (size_t)blockIdx.y * R.splits * block + (size_t)row * R.side + 4 * q;
+#pragma unroll 4
+        for (int s = g; s < R.splits; s += G) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(src + s * block));
+            acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+        }
+    }
+    if (G > 1) {
+        s_sum[threadIdx.x] = acc;
+        __syncthreads();
+        if (g != 0) return;
+        for (int i = 1; i < G; ++i) {
+            const float4 v = s_sum[i * per + pos];
+            acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+        }
+    }
+    if (!in) return;
+    float* out = R.dw + k * R.ws_k + c * R.ws_c;
+    const float v[4] = {R.alpha * acc.x, R.alpha * acc.y, R.alpha * acc.z, R.alpha * acc.w};
+    if (R.ws_c == 1 && (R.ws_k & 3) == 0) *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[2], v[3]);
+    else
+        for (int e = 0; e < 4; ++e) if (c + e < R.c) out[e * R.ws_c] = v[e];
+}
+
+// ---------------------------------------------------------------- host side
+int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+int round_up(int v, int m) { return (v + m - 1) / m * m; }
+
+struct PackedHost { int cg, f32, pack, npqk, full, splits, units, grid, chunks, tiles_c, tail; };
+static_assert(sizeof(PackedHost) <= sizeof(((PackedPlan*)nullptr)->opaque), "opaque");
+
+template <int CG, int PLANES>
+cudaError_t launch(const CUtensorMap& map_dy, const CUtensorMap& map_x, const PackedParams& P, int format, int grid, cudaStream_t stream)
+{
+    auto kern = format == GACONV_ACT_E4M3 ? packed_dw_kernel<CG, PLANES, GACONV_ACT_E4M3> : packed_dw_kernel<CG, PLANES, GACONV_ACT_INT8>;
+    static std::atomic<unsigned long long> ready[2];
+    const cudaError_t err = allow_shared_memory((const void*)kern, ready[format]);
+    if (err != cudaSuccess) return err;
+    return launch_kernel(kern, dim3((unsigned)grid), dim3(kThreads), (size_t)Config<CG, PLANES>::bytes + 1024, stream, dim3(CG, 1, 1), map_dy, map_x, P);
+}
+
+}  // namespace
+
+// Tiles of 256 x 256 by CTA pairs where they leave the GPU less idle than tiles of 128 x 128, splits where tiles are few.
+// The estimate counts cycles: stages, and what a round and a split cost beside them.
+bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan)
+{
+    if (g.r != 1 || g.s != 1 || g.stride_h != 1 || g.stride_w != 1 || g.pad_h != 0 || g.pad_w != 0) return false;
+    const long long rows = (long long)g.n * g.p * g.q;
+    if (rows > 0x7fffff00ll || !tensor_maps_available()) return false;
+    PackedHost best{};
+    double best_cost = 0;
+    const int sms = g.sm_budget > 0 ? std::min(g.sm_budget, device_sms()) : device_sms();
+    const bool last = dy_npqk || g.k == 1 || g.p * g.q == 1;
+    const bool pack = !g.bf16 || g.k % 8 != 0 || !last;
+    if (pack && rows * round_up(g.k, 8) > 0x7fffffffll) return false;
+    for (int cg = 1; cg <= (g.bf16 ? 2 : 1); ++cg) {
+        PackedHost H{};
+        H.cg = cg; H.f32 = !g.bf16; H.pack = pack; H.npqk = last;
+        H.chunks = (int)((rows + kRows - 1) / kRows);
+        H.tiles_c = ceil_div(g.c, 128 * cg);
+        const long long tiles = (long long)H.tiles_c * ceil_div(g.k, 128 * cg);
+        if (tiles > 1 << 24) continue;
+        const int clusters = std::max(1, sms / cg);
+        const double stage = cg == 2 ? 700 : H.f32 ? 1100 : 560, fixed = 4000, block = 128.0 * 128 * cg * 4 / 20;
+        H.full = (int)(tiles / clusters * clusters);
+        const int tail = (int)(tiles - H.full);
+        for (int s = 1; s <= std::min(H.chunks, std::max(1, tail == 0 ? 1 : 4 * clusters / std::max(1, tail))); ++s) {
+            const double rounds = std::ceil((double)tail * s / clusters);
+            double cost = (double)(H.full / clusters) * H.chunks * stage + rounds * (ceil_div(H.chunks, s) * stage + 600) + fixed + block;
+            if (s > 1) cost += 3000 + (double)tail * s * 128 * 128 * cg * cg * 4 / (clusters * cg) / 20;
+            if (best.units != 0 && cost >= best_cost) continue;
+            best_cost = cost;
+            H.splits = s; H.tail = tail;
+            H.units = H.full + tail * s;
+            H.grid = std::min(H.units, clusters) * cg;
+            best = H;
+        }
+    }
+    if (best.units == 0) return false;
+    plan->partial_bytes = best.splits == 1 ? 0 : align_up((size_t)best.tail * best.splits * (128 * best.cg) * (128 * best.cg) * sizeof(float) + 256, 256);
+    plan->dy_bytes = pack ? align_up((size_t)rows * round_up(g.k, 8) * (g.bf16 ? 2 : 6), 256) : 0;
+    memcpy(plan->opaque, &best, sizeof(best));
+    return true;
+}
+
+cudaError_t launch_packed(const void* codes, const void* scales, int format, const void* dy, float* dw, float* partial, void* dy_scratch, uint32_t* status, const Geom& g,
+                          const PackedPlan& plan, cudaStream_t stream)
+{
+    PackedHost H;
+    memcpy(&H, plan.opaque, sizeof(H));
+    PackedParams P{};
+    partial = reinterpret_cast<float*>(align_up(reinterpret_cast<size_t>(partial), 256));          // (a workspace starts on 16 bytes)
+    P.scales = static_cast<const uint8_t*>(scales);
+    P.dw = dw; P.partial = partial; P.status = status;
+    P.rows = (int)((long long)g.n * g.p * g.q); P.c = g.c; P.k = g.k; P.groups = act_groups(g.c);
+    P.ws_k = g.ws_k; P.ws_c = g.ws_c; P.alpha = g.alpha;
+    P.tiles_c = H.tiles_c; P.full = H.full; P.splits = H.splits; P.units = H.units; P.chunks = H.chunks;
+    const int kp = H.pack ? round_up(g.k, 8) : g.k, planes = H.f32 ? 3 : 1;
+    cudaError_t err;
+    if (H.pack) {
+        if ((err = launch_pack_rows(dy, dy_scratch, g.k, kp, g.p * g.q, g.n, H.npqk != 0, H.f32 != 0, stream)) != cudaSuccess) return err;
+        dy = dy_scratch;
+    }
+    auto encode = [&](CUtensorMap* map, CUtensorMapDataType type, const void* at, int ch, size_t pitch, int third, cuuint32_t box_ch, CUtensorMapSwizzle swz) {
+        const cuuint64_t dims[3] = {(cuuint64_t)ch, (cuuint64_t)P.rows, (cuuint64_t)third}, strides[2] = {pitch, third > 1 ? pitch * P.rows : pitch};
+        const cuuint32_t box[3] = {box_ch, kRows, 1}, es[3] = {1, 1, 1};
+        return encode_fn()(map, type, 3, const_cast<void*>(at), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    CUtensorMap map_dy, map_x;
+    if (!encode(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, g.k, (size_t)kp * 2, planes, 64, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !encode(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, act_pitch(g.c), act_pitch(g.c), 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE))
+        return cudaErrorInvalidValue;
+    err = H.f32 ? launch<1, 3>(map_dy, map_x, P, format, H.grid, stream) : H.cg == 2 ? launch<2, 1>(map_dy, map_x, P, format, H.grid, stream)
+                : launch<1, 1>(map_dy, map_x, P, format, H.grid, stream);
+    if (err != cudaSuccess) return err;
+    note_launch();
+    if (H.splits == 1) return cudaSuccess;
+    PackedReduce R{partial, dw, g.ws_k, g.ws_c, g.alpha, g.c, g.k, 128 * H.cg, H.tiles_c, H.full, H.splits, 0};
+    while (R.log_g < 5 && 4 << R.log_g < H.splits) ++R.log_g;
+    const int quads = R.side * R.side / 4, per = 256 >> R.log_g;
+    err = launch_kernel(packed_reduce_kernel, dim3((unsigned)(quads / per), (unsigned)H.tail), dim3(256), 0, stream, dim3(1, 1, 1), R);
+    if (err == cudaSuccess) note_launch();
+    return err;
+}
+
+}  // namespace gaconv
