@@ -37,20 +37,23 @@
 namespace gaconv {
 namespace {
 
-constexpr int kRows = 64;                           // rows t of a stage
-constexpr int kTile = kRows * 128;                  // bytes of 64 channels of a stage
-constexpr int kRaw = kRows * 128 + kRows * 8;       // 128 channels in 8 bits, and the two words around the four scales of each row
-constexpr int kThreads = 640;                       // warps 0-3: copies of dY, MMAs, copies of X and scales, scales; 4-11 turn X, 12-19 sum
-constexpr int kMaxDy = 6, kMaxRaw = 7, kTurned = 3;    // stages of dY, of X in 8 bits, of X turned
+constexpr int kRows = 64;                           // rows t that are turned, and multiplied, at a time
+constexpr int kTile = kRows * 128;                  // bytes of 64 channels of them in bf16
+constexpr int kThreads = 640;                       // warps 0-3: scales, MMAs, copies of X, copies of dY; 4-11 turn X, 12-19 sum
+constexpr int kMaxRing = 4;
 
+// Three rings: dY and X in 8 bits as they are copied, `halves` x 64 rows at a time (a warp takes ~500 cycles for its round of wait, byte count and copy, however
+// large the copy is, and the MMAs 512 for 64 rows), and X turned, 64 rows at a time.
 template <int CG, int PLANES> struct Config {
-    static constexpr int cols = 128 * CG, dy_stage = 2 * PLANES * kTile, dys = PLANES == 3 ? 3 : 6, raws = PLANES == 3 ? 3 : 7;
-    static constexpr int turned_at = dys * dy_stage, raw_at = turned_at + kTurned * 2 * kTile, bytes = raw_at + raws * kRaw;
-    static constexpr int epoch = PLANES == 3 ? 4 : 16;             // stages: chains of 48 or 64 MMAs
+    static constexpr int cols = 128 * CG, halves = PLANES == 3 ? 1 : 2, rows = halves * kRows;
+    static constexpr int dy_stage = 2 * PLANES * halves * kTile, dys = 3, turneds = PLANES == 3 ? 3 : 4, raws = 3;
+    static constexpr int raw = rows * 128 + rows * 8;               // 128 channels in 8 bits, and the two words around the four scales of each row
+    static constexpr int turned_at = dys * dy_stage, raw_at = turned_at + turneds * 2 * kTile, bytes = raw_at + raws * raw;
+    static constexpr int epoch = PLANES == 3 ? 4 : 8;               // stages of dY: chains of 48 or 64 MMAs
     // registers of a thread by role; their sum over the warps is within what the block is launched with (96 each)
-    static constexpr int regs_control = 40, regs_turn = CG == 2 ? 56 : 80, regs_sum = CG == 2 ? 160 : 104;
+    static constexpr int regs_control = 48, regs_turn = CG == 2 ? 56 : 80, regs_sum = CG == 2 ? 160 : 104;
     static_assert(4 * regs_control + 8 * regs_turn + 8 * regs_sum <= 20 * 96, "registers");
-    static_assert(dys <= kMaxDy && raws <= kMaxRaw && bytes <= 225 * 1024, "shared memory");
+    static_assert(dys <= kMaxRing && turneds <= kMaxRing && raws <= kMaxRing && bytes <= 225 * 1024, "shared memory");
 };
 
 struct PackedParams {
@@ -62,7 +65,7 @@ struct PackedParams {
     float alpha;
     int tiles_c;                                    // tile = tk * tiles_c + tc
     int full, splits, units;                        // tiles [0, full) are units of their own; the others `splits` each
-    int chunks;                                     // stages of all rows
+    int chunks;                                     // stages of dY in all rows
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
@@ -76,6 +79,13 @@ __device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity)
         if (ok) return true;
     }
     return false;
+}
+// whether a phase is over, without a wait
+__device__ __forceinline__ bool mbar_look(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
 }
 template <int CG>
 __device__ __forceinline__ void arrive_leader(uint32_t bar)
@@ -153,9 +163,8 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
 {
     typedef Config<CG, PLANES> C;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bar_full[kTurned], bar_read[kTurned], bar_dy[kMaxDy], bar_free_dy[kMaxDy], bar_raw[kMaxRaw], bar_taken[kMaxRaw], bar_acc[2], bar_free[2], bar_last;
+    __shared__ __align__(8) uint64_t bar_dy[kMaxRing], bar_free_dy[kMaxRing], bar_full[kMaxRing], bar_empty[kMaxRing], bar_raw[kMaxRing], bar_taken[kMaxRing], bar_acc[2], bar_free[2], bar_last;
     __shared__ uint32_t s_tmem;
-    __shared__ volatile int s_abort;
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -163,12 +172,11 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
 
     pdl_release_next_grid();
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kTurned; ++i) { mbar_init(smem_u32(&bar_full[i]), 4 * CG + CG - 1); mbar_init(smem_u32(&bar_read[i]), 1); }
-        for (int i = 0; i < C::dys; ++i) { mbar_init(smem_u32(&bar_dy[i]), 1); mbar_init(smem_u32(&bar_free_dy[i]), 1); }
-        for (int i = 0; i < C::raws; ++i) { mbar_init(smem_u32(&bar_raw[i]), 1 + 64); mbar_init(smem_u32(&bar_taken[i]), 4); }
+        for (int i = 0; i < C::dys; ++i) { mbar_init(smem_u32(&bar_dy[i]), rank == 0 ? CG : 1); mbar_init(smem_u32(&bar_free_dy[i]), 1); }
+        for (int i = 0; i < C::turneds; ++i) { mbar_init(smem_u32(&bar_full[i]), 4 * CG); mbar_init(smem_u32(&bar_empty[i]), 1); }
+        for (int i = 0; i < C::raws; ++i) { mbar_init(smem_u32(&bar_raw[i]), 1 + 32); mbar_init(smem_u32(&bar_taken[i]), 4 * C::halves); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bar_acc[i]), 1); mbar_init(smem_u32(&bar_free[i]), 8 * CG); }
         mbar_init(smem_u32(&bar_last), 1);
-        s_abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_dy) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_x) : "memory");
@@ -191,113 +199,150 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = s_tmem;
     pdl_wait_prior_grid();
-    auto give_up = [&] { s_abort = 1; atomicOr(P.status, 1u); };
+    auto give_up = [&] { atomicOr(P.status, 1u); };        // (the other roles' waits run out in turn)
 
     if (warp < 4) {
         regs_down<C::regs_control>();
-        if (warp == 0) {
-            // ------------------------------------------------------------ copies of dY: 64 rows x 128 outputs a stage and plane
+        if (warp == 2) {
+            // ------------------------------------------------------------ copies of X: 128 channels a stage
             Walk w;
             w.start(P, group);
             int st = 0, ph = 0, n = 0;
-            for (; w.live(); w.next(P, step), ++n) {
-                if (n >= C::dys && !pair_wait(smem_u32(&bar_free_dy[st]), ph ^ 1)) give_up();
-                if (__any_sync(0xffffffffu, s_abort)) break;
+            bool ok = true, taken = true;
+            for (; w.live(); w.next(P, step)) {
+                if (!taken) ok = mbar_wait(smem_u32(&bar_taken[st]), ph ^ 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
                 if (elect_one()) {
-                    const uint32_t bar = smem_u32(&bar_dy[st]), dst = base + st * C::dy_stage;
-                    mbar_expect_tx(bar, 2 * PLANES * kTile);
-                    const int k = (w.k0 * CG + rank) * 128, t = w.chunk * kRows;
-#pragma unroll
-                    for (int pl = 0; pl < PLANES; ++pl) {
-                        tma_load_3d(dst + 2 * pl * kTile, &map_dy, bar, k, t, pl);
-                        tma_load_3d(dst + (2 * pl + 1) * kTile, &map_dy, bar, k + 64, t, pl);
-                    }
+                    const uint32_t bar = smem_u32(&bar_raw[st]);
+                    mbar_expect_tx(bar, C::rows * 128);
+                    tma_load_3d(base + C::raw_at + st * C::raw, &map_x, bar, (w.c0 * CG + rank) * 128, w.chunk * C::rows, 0);
                 }
                 __syncwarp();
-                if (++st == C::dys) { st = 0; ph ^= 1; }
+                if (++st == C::raws) { st = 0; ph ^= 1; }
+                ++n;
+                taken = n < C::raws || mbar_look(smem_u32(&bar_taken[st]), ph ^ 1);
             }
-            // on failure the copies that were issued land; otherwise the last commits, which may come from the other CTA, arrive before this one goes (bounded)
-            const bool failed = __any_sync(0xffffffffu, s_abort);
-            for (int i = max(0, n - C::dys); i < n; ++i) pair_wait(smem_u32(failed ? &bar_dy[i % C::dys] : &bar_free_dy[i % C::dys]), (i / C::dys) & 1);
-        } else if (warp >= 2) {
-            // ------------------------------------------------------------ X in 8 bits: copies (warp 2), and scales, a row a lane of both warps
+            if (!ok) give_up();
+            // all of X that was copied has been turned; on failure the wait is the time that copies have to land (bounded)
+            for (int i = max(0, n - C::raws); i < n; ++i) mbar_wait(smem_u32(&bar_taken[i % C::raws]), (i / C::raws) & 1);
+        } else if (warp == 3) {
+            // ------------------------------------------------------------ copies of dY: 128 outputs a stage and plane, lane b issues copy b of 64
             Walk w;
             w.start(P, group);
             int st = 0, ph = 0, n = 0;
-            bool ok = true;
-            const uint8_t* end = P.scales + (long long)P.rows * P.groups;
-            for (; w.live(); w.next(P, step), ++n) {
-                if (n >= C::raws && !mbar_wait(smem_u32(&bar_taken[st]), ph ^ 1)) give_up();
-                if (__any_sync(0xffffffffu, s_abort)) { ok = false; break; }
-                const uint32_t bar = smem_u32(&bar_raw[st]), dst = base + C::raw_at + st * kRaw;
-                if (warp == 2 && elect_one()) {
-                    mbar_expect_tx(bar, kRows * 128);
-                    tma_load_3d(dst, &map_x, bar, (w.c0 * CG + rank) * 128, w.chunk * kRows, 0);
-                }
+            bool ok = true, empty = true;
+            for (; w.live(); w.next(P, step)) {
+                if (!empty) ok = pair_wait(smem_u32(&bar_free_dy[st]), ph ^ 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t bar = smem_u32(&bar_dy[st]);
+                if (lane == 0) mbar_expect_tx(bar, C::dy_stage);
                 __syncwarp();
-                // the row's scales lie on any byte: the one or two aligned words that hold them, no byte past the end
-                const int r = 32 * (warp - 2) + lane, row = w.chunk * kRows + r, g = (w.c0 * CG + rank) * 4;
-                const bool in = row < P.rows && g < P.groups;
-                const uint8_t* at = P.scales + (in ? (long long)row * P.groups + g : 0);
-                const int off = (int)(reinterpret_cast<uintptr_t>(at) & 3);
-                const ptrdiff_t left = end - (at - off);
-                const int n0 = in ? (int)min((ptrdiff_t)4, left) : 0, n1 = in && off != 0 ? (int)max((ptrdiff_t)0, min((ptrdiff_t)4, left - 4)) : 0;
-                copy_word(dst + kRows * 128 + r * 8, at - off, n0);
-                copy_word(dst + kRows * 128 + r * 8 + 4, n1 > 0 ? at - off + 4 : P.scales, n1);
+                if (lane < 2 * PLANES)
+                    tma_load_3d(base + st * C::dy_stage + lane * C::halves * kTile, &map_dy, bar, (w.k0 * CG + rank) * 128 + 64 * (lane & 1), w.chunk * C::rows, lane >> 1);
+                if (++st == C::dys) { st = 0; ph ^= 1; }
+                ++n;
+                empty = n < C::dys || mbar_look(smem_u32(&bar_free_dy[st]), ph ^ 1);
+            }
+            if (!ok) give_up();
+            // the last commits, which may come from the other CTA, arrive before this one goes; on failure the wait is the time that copies have to land (bounded)
+            for (int i = max(0, n - C::dys); i < n; ++i) pair_wait(smem_u32(&bar_free_dy[i % C::dys]), (i / C::dys) & 1);
+        } else if (warp == 0) {
+            // ------------------------------------------------------------ scales, asynchronous copies too: rows 32 apart a lane
+            Walk w;
+            w.start(P, group);
+            int st = 0, ph = 0, n = 0;
+            bool ok = true, taken = true;
+            const uint8_t* end = P.scales + (long long)P.rows * P.groups;
+            for (; w.live(); w.next(P, step)) {
+                if (!taken) ok = mbar_wait(smem_u32(&bar_taken[st]), ph ^ 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t bar = smem_u32(&bar_raw[st]), dst = base + C::raw_at + st * C::raw + C::rows * 128;
+                const int g = (w.c0 * CG + rank) * 4;
+#pragma unroll
+                for (int i = 0; i < C::rows / 32; ++i) {
+                    // a row's scales lie on any byte: the one or two aligned words that hold them, no byte past the end
+                    const int r = 32 * i + lane, row = w.chunk * C::rows + r;
+                    const bool in = row < P.rows && g < P.groups;
+                    const uint8_t* at = P.scales + (in ? (long long)row * P.groups + g : 0);
+                    const int off = (int)(reinterpret_cast<uintptr_t>(at) & 3);
+                    const int left = (int)min((ptrdiff_t)8, end - (at - off));
+                    copy_word(dst + r * 8, at - off, in ? min(4, left) : 0);
+                    if ((P.groups & 3) != 0) copy_word(dst + r * 8 + 4, in && off != 0 && left > 4 ? at - off + 4 : P.scales, in && off != 0 ? max(0, left - 4) : 0);
+                }
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
                 if (++st == C::raws) { st = 0; ph ^= 1; }
+                ++n;
+                taken = n < C::raws || mbar_look(smem_u32(&bar_taken[st]), ph ^ 1);
             }
-            if (!ok) asm volatile("cp.async.wait_all;" ::: "memory");
-            if (!ok && warp == 2)        // the copies that were issued land (bounded; the other warp's share of the last barrier may be missing)
-                for (int i = max(0, n - C::raws); i < n; ++i) mbar_wait(smem_u32(&bar_raw[i % C::raws]), (i / C::raws) & 1);
+            if (!ok) { give_up(); asm volatile("cp.async.wait_all;" ::: "memory"); }
         } else if (CG == 2 && warp == 1 && rank == 1) {
             // ------------------------------------------------------------ tells the leader of this CTA's copies of dY
             Walk w;
             w.start(P, group);
-            int st = 0, ds = 0, dph = 0;
+            int st = 0, ph = 0;
             for (; w.live(); w.next(P, step)) {
-                if (!mbar_wait(smem_u32(&bar_dy[ds]), dph)) give_up();
-                if (__any_sync(0xffffffffu, s_abort)) break;
-                if (lane == 0) arrive_leader<CG>(smem_u32(&bar_full[st]));
-                if (++st == kTurned) st = 0;
-                if (++ds == C::dys) { ds = 0; dph ^= 1; }
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_dy[st]), ph))) { give_up(); break; }
+                if (lane == 0) arrive_leader<CG>(smem_u32(&bar_dy[st]));
+                if (++st == C::dys) { st = 0; ph ^= 1; }
             }
         } else if (warp == 1 && rank == 0) {
             // ------------------------------------------------------------ MMAs
             // M = 128 a CTA, N = cols; bf16 operands, both MN-major, fp32 accumulators
             constexpr uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(C::cols / 8) << 17 | (uint32_t)(8 * CG) << 24;
             constexpr uint64_t hi = (uint64_t)(1024 / 16 | 1u << 14 | 2u << 29) << 32;          // eight rows to the next, 128-byte swizzle
-            constexpr uint32_t lbo = (uint32_t)(kTile / 16) << 16;                              // 64 channels to the next
+            constexpr uint32_t lbo_dy = (uint32_t)(C::halves * kTile / 16) << 16, lbo_x = (uint32_t)(kTile / 16) << 16;         // 64 channels to the next
+            // A look at a barrier takes ~200 cycles even where the phase is over, so the next stage's is looked at before this one's MMAs are issued.
             Walk w;
             w.start(P, group);
-            int st = 0, ph = 0, ds = 0, dph = 0, set = 0, in_epoch = 0, epochs = 0;
-            while (w.live()) {
-                if (in_epoch == 0 && epochs >= 2 && !pair_wait(smem_u32(&bar_free[set]), ((epochs >> 1) - 1) & 1)) give_up();
-                if (!s_abort && !(mbar_wait(smem_u32(&bar_dy[ds]), dph) && pair_wait(smem_u32(&bar_full[st]), ph))) give_up();
-                if (__any_sync(0xffffffffu, s_abort)) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const bool ends = w.left == 1 || in_epoch + 1 == C::epoch;
-                if (elect_one()) {
-                    const uint32_t a0 = base + ds * C::dy_stage, b0 = base + C::turned_at + st * 2 * kTile;
-                    const uint64_t a = hi | (lbo | (a0 >> 4)), b = hi | (lbo | (b0 >> 4));
-                    const uint32_t d = tmem + set * C::cols;
+            int st = 0, ph = 0, ds = 0, dph = 0, set = 0, epochs = 0;
+            bool ready = false, ready_dy = false, ok = true;
+            while (ok && w.live()) {
+                int in_epoch = 0;
+                for (int left = w.left; left > 0; --left) {
+                    if (in_epoch == 0 && epochs >= 2) ok = pair_wait(smem_u32(&bar_free[set]), ((epochs >> 1) - 1) & 1);
+                    if (!ready_dy) ok = ok && pair_wait(smem_u32(&bar_dy[ds]), dph);
+                    const int next_ds = ds + 1 == C::dys ? 0 : ds + 1;
+                    dph ^= next_ds == 0 ? 1 : 0;
+                    const bool ends = left == 1 || in_epoch + 1 == C::epoch;
 #pragma unroll
-                    for (int i = 0; i < kRows / 16; ++i)
+                    for (int h = 0; h < C::halves; ++h) {
+                        if (!ready) ok = ok && pair_wait(smem_u32(&bar_full[st]), ph);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const int next = st + 1 == C::turneds ? 0 : st + 1;
+                        ph ^= next == 0 ? 1 : 0;
+                        ready = mbar_look(smem_u32(&bar_full[next]), ph);
+                        if (h == C::halves - 1) ready_dy = mbar_look(smem_u32(&bar_dy[next_ds]), dph);
+                        if (elect_one()) {
+                            const uint32_t a0 = base + ds * C::dy_stage + h * kTile, b0 = base + C::turned_at + st * 2 * kTile;
+                            const uint64_t a = hi | (lbo_dy | (a0 >> 4)), b = hi | (lbo_x | (b0 >> 4));
+                            const uint32_t d = tmem + set * C::cols;
 #pragma unroll
-                        for (int pl = PLANES - 1; pl >= 0; --pl)
-                            mma<CG>(d, a + (pl * 2 * kTile + i * 2048) / 16, b + i * 2048 / 16, idesc, in_epoch > 0 || i > 0 || pl < PLANES - 1 ? 1u : 0u);
-                    commit<CG>(smem_u32(&bar_read[st]));
-                    commit<CG>(smem_u32(&bar_free_dy[ds]));
-                    if (ends) commit<CG>(smem_u32(&bar_acc[set]));
+                            for (int i = 0; i < kRows / 16; ++i)
+#pragma unroll
+                                for (int pl = PLANES - 1; pl >= 0; --pl)
+                                    mma<CG>(d, a + (pl * 2 * C::halves * kTile + i * 2048) / 16, b + i * 2048 / 16, idesc, in_epoch > 0 || h > 0 || i > 0 || pl < PLANES - 1 ? 1u : 0u);
+                            commit<CG>(smem_u32(&bar_empty[st]));
+                            if (h == C::halves - 1) commit<CG>(smem_u32(&bar_free_dy[ds]));
+                            if (h == C::halves - 1 && ends) commit<CG>(smem_u32(&bar_acc[set]));
+                        }
+                        __syncwarp();
+                        st = next;
+                    }
+                    if (!ok) break;
+                    ++in_epoch;
+                    if (ends) { in_epoch = 0; set ^= 1; ++epochs; }
+                    ds = next_ds;
                 }
-                __syncwarp();
-                ++in_epoch;
-                if (ends) { in_epoch = 0; set ^= 1; ++epochs; }
-                if (++st == kTurned) { st = 0; ph ^= 1; }
-                if (++ds == C::dys) { ds = 0; dph ^= 1; }
-                w.next(P, step);
+                w.unit += step;
+                w.enter(P);
             }
-            if (__any_sync(0xffffffffu, s_abort)) {      // the MMAs that were issued end (bounded)
+            if (!ok) {      // the MMAs that were issued end (bounded)
+                give_up();
                 if (elect_one()) {
                     if (CG == 2) asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&bar_last)) : "memory");
                     else umma_commit(smem_u32(&bar_last));
@@ -308,32 +353,41 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
         }
     } else if (warp < 12) {
         // ---------------------------------------------------------------- X: 8 bits -> bf16
-        // Four warps take a stage, the other four the next.  A thread turns pieces of 16 channels, chunk q of rows `row` + 16 i.  Eight lanes take the
+        // Four warps take 64 rows, the other four the next.  A thread turns pieces of 16 channels, chunk q of rows `row` + 16 i.  Eight lanes take the
         // lower 64 channels of a row and the upper 64 of its neighbour: then neither their reads nor their writes, whose chunks are permuted by
         // the row, meet in a bank.
         regs_down<C::regs_turn>();
         const int t = threadIdx.x & 127, mine = (warp - 4) >> 2, q = t & 7, row = (t >> 3) ^ (q >> 2);
-        const uint32_t from = base + C::raw_at + row * 128 + 16 * q;
+        constexpr int advance = 2 / C::halves;          // stages from this group's rows to its next
+        const uint32_t raw = base + C::raw_at, half = C::halves == 2 ? mine * kRows : 0;
+        const uint32_t from = raw + (half + row) * 128 + 16 * q;
         // (a row's first scale lies at byte (row * groups) % 4 of its two words, the same for rows 4 apart)
-        const uint32_t scale = base + C::raw_at + kRows * 128 + row * 8 + (row * P.groups & 3) + (q >> 1);
+        const uint32_t scale = raw + C::rows * 128 + (half + row) * 8 + (row * P.groups & 3) + (q >> 1);
         const uint32_t to = base + C::turned_at + (q >> 2) * kTile + row * 128, x0 = ((2 * (q & 3)) ^ (row & 7)) << 4;
         Walk w;
         w.start(P, group);
-        if (mine == 1 && w.live()) w.next(P, step);
-        int st = mine, ph = 0, rs = mine, rph = 0, n = mine;
-        bool ok = true;
+        if (C::halves == 1 && mine == 1 && w.live()) w.next(P, step);
+        int st = mine, ph = 0, rs = C::halves == 1 ? mine : 0, rph = 0, n = mine;
+        bool ok = true, filled = false, empty = true;
         while (w.live()) {
-            if (!mbar_wait(smem_u32(&bar_raw[rs]), rph)) give_up();
+            if (!filled) ok = mbar_wait(smem_u32(&bar_raw[rs]), rph);
             uint4 v[4];
             uint32_t s[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                v[i] = load_shared16(from + rs * kRaw + i * 2048);
-                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(s[i]) : "r"(scale + rs * kRaw + i * 128) : "memory");
+                v[i] = load_shared16(from + rs * C::raw + i * 2048);
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(s[i]) : "r"(scale + rs * C::raw + i * 128) : "memory");
             }
-            if (n >= kTurned && !pair_wait(smem_u32(&bar_read[st]), ph ^ 1)) give_up();
-            if (__any_sync(0xffffffffu, s_abort)) { ok = false; break; }
+            if (!empty) ok = ok && pair_wait(smem_u32(&bar_empty[st]), ph ^ 1);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
             const uint32_t dst = to + st * 2 * kTile;
+            const int old_st = st, old_rs = rs;
+            for (st += 2; st >= C::turneds; st -= C::turneds) ph ^= 1;
+            for (rs += advance; rs >= C::raws; rs -= C::raws) rph ^= 1;
+            n += 2;
+            filled = mbar_look(smem_u32(&bar_raw[rs]), rph);
+            empty = n < C::turneds || mbar_look(smem_u32(&bar_empty[st]), ph ^ 1);
             const bool rest = __any_sync(0xffffffffu, act_has_rest<FMT>(max(max(s[0], s[1]), max(s[2], s[3]))));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -349,16 +403,14 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) { arrive_leader<CG>(smem_u32(&bar_full[st])); arrive(smem_u32(&bar_taken[rs])); }
-            for (st += 2; st >= kTurned; st -= kTurned) ph ^= 1;
-            for (rs += 2; rs >= C::raws; rs -= C::raws) rph ^= 1;
-            n += 2;
+            if (lane == 0) { arrive_leader<CG>(smem_u32(&bar_full[old_st])); arrive(smem_u32(&bar_taken[old_rs])); }
             w.next(P, step);
-            if (w.live()) w.next(P, step);
+            if (C::halves == 1 && w.live()) w.next(P, step);
         }
+        if (!ok) give_up();
         // the last commits have arrived before this CTA goes (bounded; they may come from the other one)
         if (ok && (warp & 3) == 0)
-            for (int i = n - 2; i >= 0 && i + kTurned >= n; i -= 2) pair_wait(smem_u32(&bar_read[i % kTurned]), (i / kTurned) & 1);
+            for (int i = n - 2; i >= 0 && i + C::turneds >= n; i -= 2) pair_wait(smem_u32(&bar_empty[i % C::turneds]), (i / C::turneds) & 1);
     } else {
         // ---------------------------------------------------------------- sums
         // Warps w and w + 4 share 32 lanes of tensor memory (outputs) and take half of the columns (channels) each.
@@ -376,11 +428,9 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
             bool fresh = true;
             for (; left > 0; left -= C::epoch) {
                 const int set = epochs & 1;
-                ok = pair_wait(smem_u32(&bar_acc[set]), (epochs >> 1) & 1);
-                if (!ok) give_up();
-                ok = __all_sync(0xffffffffu, ok && !s_abort);
+                ok = __all_sync(0xffffffffu, pair_wait(smem_u32(&bar_acc[set]), (epochs >> 1) & 1));
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (!ok) break;
+                if (!ok) { give_up(); break; }
                 const uint32_t src = tmem + set * C::cols + half * H + ((uint32_t)(32 * sp) << 16);
                 if (fresh) {
 #pragma unroll
@@ -528,12 +578,13 @@ bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan)
     for (int cg = 1; cg <= (g.bf16 ? 2 : 1); ++cg) {
         PackedHost H{};
         H.cg = cg; H.f32 = !g.bf16; H.pack = pack; H.npqk = last;
-        H.chunks = (int)((rows + kRows - 1) / kRows);
+        const int stage_rows = g.bf16 ? Config<1, 1>::rows : Config<1, 3>::rows;
+        H.chunks = (int)((rows + stage_rows - 1) / stage_rows);
         H.tiles_c = ceil_div(g.c, 128 * cg);
         const long long tiles = (long long)H.tiles_c * ceil_div(g.k, 128 * cg);
         if (tiles > 1 << 24) continue;
         const int clusters = std::max(1, sms / cg);
-        const double stage = cg == 2 ? 700 : H.f32 ? 1100 : 560, fixed = 4000, block = 128.0 * 128 * cg * 4 / 20;
+        const double stage = cg == 2 ? 1250 : 1000, fixed = 4000, block = 128.0 * 128 * cg * 4 / 20;
         H.full = (int)(tiles / clusters * clusters);
         const int tail = (int)(tiles - H.full);
         for (int s = 1; s <= std::min(H.chunks, std::max(1, tail == 0 ? 1 : 4 * clusters / std::max(1, tail))); ++s) {
@@ -574,8 +625,9 @@ cudaError_t launch_packed(const void* codes, const void* scales, int format, con
         dy = dy_scratch;
     }
     auto encode = [&](CUtensorMap* map, CUtensorMapDataType type, const void* at, int ch, size_t pitch, int third, cuuint32_t box_ch, CUtensorMapSwizzle swz) {
+        const cuuint32_t stage_rows = H.f32 ? Config<1, 3>::rows : Config<1, 1>::rows;
         const cuuint64_t dims[3] = {(cuuint64_t)ch, (cuuint64_t)P.rows, (cuuint64_t)third}, strides[2] = {pitch, third > 1 ? pitch * P.rows : pitch};
-        const cuuint32_t box[3] = {box_ch, kRows, 1}, es[3] = {1, 1, 1};
+        const cuuint32_t box[3] = {box_ch, stage_rows, 1}, es[3] = {1, 1, 1};
         return encode_fn()(map, type, 3, const_cast<void*>(at), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
