@@ -91,93 +91,28 @@ __device__ __forceinline__ uint32_t act_scale2(uint32_t byte)
 }
 template <int FMT> __device__ __forceinline__ bool act_has_rest(uint32_t byte) { return FMT == GACONV_ACT_E4M3 && byte > 134; }
 __device__ __forceinline__ uint32_t act_rest2(uint32_t byte) { return byte == 255 ? 0x7fc07fc0u : byte > 134 ? (byte - 134 + 127) * 0x00800080u : 0x3f803f80u; }
-// eight codes
-template <int FMT>
-__device__ __forceinline__ uint4 act_decode8(uint2 q, uint32_t byte)
-{
-    const uint32_t s2 = act_scale2<FMT>(byte);
-    const uint2 a = act_decode4<FMT>(q.x, s2), b = act_decode4<FMT>(q.y, s2);
-    uint4 v = make_uint4(a.x, a.y, b.x, b.y);
-    if (act_has_rest<FMT>(byte)) {
-        const uint32_t r = act_rest2(byte);
-        v = make_uint4(bf2_mul(v.x, r), bf2_mul(v.y, r), bf2_mul(v.z, r), bf2_mul(v.w, r));
-    }
-    return v;
-}
-
-// ---- eight neighbouring elements of a row as fp32 ----
-// VEC: the eight lie on a 16-byte boundary, otherwise they are read or written one by one; `left`: how many of them the row has
-template <bool VEC>
-__device__ __forceinline__ void load8(const float* p, int left, float (&v)[8])
-{
-    if (VEC && left >= 8) {
-        const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.f;
-    }
-}
-template <bool VEC>
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, int left, float (&v)[8])
-{
-    if (VEC && left >= 8) {
-        const uint4 t = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < left ? __bfloat162float(p[i]) : 0.f;
-    }
-}
-template <bool VEC>
-__device__ __forceinline__ void store8(float* p, int left, const float (&v)[8])
-{
-    if (VEC && left >= 8) {
-        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < left) p[i] = v[i];
-    }
-}
-template <bool VEC>
-__device__ __forceinline__ void store8(__nv_bfloat16* p, int left, const float (&v)[8])
-{
-    if (VEC && left >= 8) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&t);
-        }
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < left) p[i] = __float2bfloat16_rn(v[i]);
-    }
-}
-// the value that an element of the type has
-__device__ __forceinline__ float rounded(float v, const float*) { return v; }
-__device__ __forceinline__ float rounded(float v, const __nv_bfloat16*) { return __bfloat162float(__float2bfloat16_rn(v)); }
-
-// Quantises eight elements; the four lanes of an aligned quartet hold the 32 channels of a group and call together (elements past the row: 0).
-// Writes the codes, and from the quartet's first lane the scale.  codes: the row's, at the eight; `pitch_left`: bytes of the row from there.
-template <int FMT>
-__device__ __forceinline__ void act_store8(const float (&v)[8], uint8_t* codes, int pitch_left, uint8_t* scale, bool first)
+// Quantises N neighbouring elements; the 32 / N lanes of an aligned group of lanes hold the 32 channels of a group and call together, all lanes of
+// the warp (elements past the row: 0).  Writes the codes, and from the first of these lanes the scale.  codes: the row's, at the elements;
+// `pitch_left`: bytes of the row from there.
+template <int FMT, int N>
+__device__ __forceinline__ void act_store(const float (&v)[N], uint8_t* codes, int pitch_left, uint8_t* scale, bool first)
 {
     uint32_t a = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(v[i]) & 0x7fffffffu);
-    a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
-    a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
+    for (int i = 0; i < N; ++i) a = max(a, __float_as_uint(v[i]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = 1; o < 32 / N; o *= 2) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
     if (pitch_left <= 0) return;
     const int byte = act_scale_byte<FMT>(a);
     const float inv = act_inverse(byte);
-    uint2 q = make_uint2(act_encode4<FMT>(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv), act_encode4<FMT>(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
-    if (byte == 255) q = make_uint2(0, 0);
-    *reinterpret_cast<uint2*>(codes) = q;
+    uint32_t q[N / 4];
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        q[i] = act_encode4<FMT>(v[4 * i] * inv, v[4 * i + 1] * inv, v[4 * i + 2] * inv, v[4 * i + 3] * inv);
+        if (byte == 255) q[i] = 0;
+    }
+    if constexpr (N == 8) *reinterpret_cast<uint2*>(codes) = make_uint2(q[0], q[1]);
+    else *reinterpret_cast<uint32_t*>(codes) = q[0];
     if (first) *scale = (uint8_t)byte;
 }
 

@@ -46,13 +46,15 @@ constexpr int kMaxRing = 4;
 // large the copy is, and the MMAs 512 for 64 rows), and X turned, 64 rows at a time.
 template <int CG, int PLANES> struct Config {
     static constexpr int cols = 128 * CG, halves = PLANES == 3 ? 1 : 2, rows = halves * kRows;
-    static constexpr int dy_stage = 2 * PLANES * halves * kTile, dys = 3, turneds = PLANES == 3 ? 3 : 4, raws = 3;
+    static constexpr int dy_stage = 2 * PLANES * halves * kTile, dys = 3, turneds = PLANES == 3 ? 2 : 4, raws = PLANES == 3 ? 4 : 3;
     static constexpr int raw = rows * 128 + rows * 8;               // 128 channels in 8 bits, and the two words around the four scales of each row
     static constexpr int turned_at = dys * dy_stage, raw_at = turned_at + turneds * 2 * kTile, bytes = raw_at + raws * raw;
     static constexpr int epoch = PLANES == 3 ? 4 : 8;               // stages of dY: chains of 48 or 64 MMAs
     // registers of a thread by role; their sum over the warps is within what the block is launched with (96 each)
     static constexpr int regs_control = 48, regs_turn = CG == 2 ? 56 : 80, regs_sum = CG == 2 ? 160 : 104;
     static_assert(4 * regs_control + 8 * regs_turn + 8 * regs_sum <= 20 * 96, "registers");
+    // A wait for a phase is only right once the phase before is over, which a group knows of its own stages alone: no slot passes from one group to the other
+    static_assert(turneds % 2 == 0 && raws * halves % 2 == 0, "two groups turn X");
     static_assert(dys <= kMaxRing && turneds <= kMaxRing && raws <= kMaxRing && bytes <= 225 * 1024, "shared memory");
 };
 
@@ -74,7 +76,7 @@ __device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity)
 {
     for (uint32_t i = 0; i < kWaitLimit; ++i) {
         uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
         if (ok) return true;
     }
@@ -84,7 +86,7 @@ __device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity)
 __device__ __forceinline__ bool mbar_look(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
 template <int CG>

@@ -3,7 +3,7 @@
 //   forward    s = x + r (rounded to the type),  rstd = 1 / sqrt(mean(s^2) + eps),  y = s rstd w (rounded once),  codes, scales = y in 8 bits (act8.cuh)
 //   backward   h = s rstd,  g = dy w,  dx = ds + rstd (g - h mean(g h)),  dw = sum over rows of dy h
 //
-// Bound by HBM: every tensor is read and written once.  A team of `lanes` threads holds a row in registers, `NU` pieces of eight channels a
+// Bound by HBM: every tensor is read and written once.  A team of `lanes` threads holds a row in registers, `NU` pieces of 16 bytes (rows.cuh) a
 // thread, so that the second use of a row (after its mean) reads nothing.  Sums and means are fp32, in an order that depends on the sizes alone.
 #include <algorithm>
 #include <type_traits>
@@ -11,6 +11,7 @@
 #include "act8.cuh"
 #include "device_utils.cuh"
 #include "gaconv_internal.h"
+#include "rows.cuh"
 
 namespace gaconv {
 namespace {
@@ -31,19 +32,31 @@ __device__ __forceinline__ float team_sum(float v, int log_lanes, float (*part)[
     return v;
 }
 
-template <typename T> __device__ __forceinline__ float act_type_round(float v) { return rounded(v, static_cast<const T*>(nullptr)); }
-
-__device__ __forceinline__ void store_codes(const NormRows& o, const float (&t)[8], uint8_t* codes, uint8_t* scales, long long r, int c, int pitch_left)
+template <int N>
+__device__ __forceinline__ void store_codes(const NormRows& o, const float (&t)[N], uint8_t* codes, uint8_t* scales, long long r, int c, int pitch_left)
 {
     uint8_t *q = codes + r * o.pitch + c, *s = scales + r * o.groups + (c >> 5);
-    if (o.format == GACONV_ACT_E4M3) act_store8<GACONV_ACT_E4M3>(t, q, pitch_left, s, (c & 31) == 0);
-    else act_store8<GACONV_ACT_INT8>(t, q, pitch_left, s, (c & 31) == 0);
+    if (o.format == GACONV_ACT_E4M3) act_store<GACONV_ACT_E4M3, N>(t, q, pitch_left, s, (c & 31) == 0);
+    else act_store<GACONV_ACT_INT8, N>(t, q, pitch_left, s, (c & 31) == 0);
 }
+// x + r, rounded to the type
+template <typename T>
+__device__ __forceinline__ uint4 add_pieces(const uint4& x, const uint4& r)
+{
+    float a[kPiece<T>], b[kPiece<T>];
+    to_floats<T>(x, a); to_floats<T>(r, b);
+#pragma unroll
+    for (int j = 0; j < kPiece<T>; ++j) a[j] += b[j];
+    return from_floats<T>(a);
+}
+template <typename T>
+__device__ __forceinline__ const T* end_of(const T* p, const NormRows& o, long long stride) { return p + (o.rows - 1) * stride + o.cols; }
 
 template <typename T, int NU, bool VEC>
 __global__ void __launch_bounds__(512)
 rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __restrict__ w, T* sum, T* y, uint8_t* codes, uint8_t* scales, float* rstd, int log_lanes)
 {
+    constexpr int N = kPiece<T>;
     __shared__ float part[2][16];
     pdl_release_next_grid();
     const int lanes = 1 << log_lanes, l = threadIdx.x & (lanes - 1);
@@ -51,42 +64,58 @@ rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __re
     const bool live = row < o.rows;          // (teams without a row go along: shuffles and barriers are shared)
     const long long r = live ? row : 0;
     const int cols = live ? o.cols : 0;
+    const T *xr = x + r * o.x_stride, *rr = res + r * o.r_stride, *x_end = end_of(x, o, o.x_stride), *r_end = end_of(res, o, o.r_stride);
     int turn = 0;
     pdl_wait_prior_grid();
-    float v[NU][8];
-#pragma unroll
-    for (int i = 0; i < NU; ++i) load8<VEC>(x + r * o.x_stride + 8 * (i * lanes + l), cols - 8 * (i * lanes + l), v[i]);
-    if (res != nullptr) {
+    uint4 v[NU];
+    {
+        Piece<T, VEC> px[NU], pr[NU];
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            float t[8];
-            load8<VEC>(res + r * o.r_stride + 8 * (i * lanes + l), cols - 8 * (i * lanes + l), t);
+            const int c = N * (i * lanes + l);
+            px[i].start(xr + c, cols - c, x_end);
+            if (res != nullptr) pr[i].start(rr + c, cols - c, r_end);
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = act_type_round<T>(v[i][j] + t[j]);
+        for (int i = 0; i < NU; ++i) {
+            const int c = N * (i * lanes + l);
+            v[i] = px[i].value(xr + c, cols - c, x_end);
+            if (res != nullptr) v[i] = add_pieces<T>(v[i], pr[i].value(rr + c, cols - c, r_end));
         }
     }
     if (sum != nullptr) {
 #pragma unroll
-        for (int i = 0; i < NU; ++i) store8<VEC>(sum + r * o.s_stride + 8 * (i * lanes + l), cols - 8 * (i * lanes + l), v[i]);
+        for (int i = 0; i < NU; ++i) store_piece<T, VEC>(sum + r * o.s_stride + N * (i * lanes + l), cols - N * (i * lanes + l), v[i], log_lanes);
     }
     float q = 0.f;
 #pragma unroll
-    for (int i = 0; i < NU; ++i)
+    for (int i = 0; i < NU; ++i) {
+        float f[N], t = 0.f;
+        to_floats<T>(v[i], f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q = fmaf(v[i][j], v[i][j], q);
+        for (int j = 0; j < N; ++j) t = fmaf(f[j], f[j], t);
+        q += t;
+    }
     q = team_sum(q, log_lanes, part, turn);
     const float rs = 1.f / sqrtf(q / (float)o.cols + o.eps);
     if (live && l == 0 && rstd != nullptr) rstd[r] = rs;
     const int pitch = live ? o.pitch : 0;
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-        const int c = 8 * (i * lanes + l);
-        float t[8];
-        load8<true>(w + c, o.cols - c, t);
+        const int c = N * (i * lanes + l);
+        float f[N], t[N];
+        Piece<T, true> pw;
+        pw.start(w + c, o.cols - c, nullptr);
+        to_floats<T>(pw.value(w + c, o.cols - c, nullptr), t);
+        to_floats<T>(v[i], f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] = act_type_round<T>(v[i][j] * rs * t[j]);
-        if (y != nullptr) store8<VEC>(y + r * o.y_stride + c, cols - c, t);
-        if (codes != nullptr) store_codes(o, t, codes, scales, r, c, pitch - c);
+        for (int j = 0; j < N; ++j) t[j] = f[j] * rs * t[j];
+        const uint4 out = from_floats<T>(t);
+        if (y != nullptr) store_piece<T, VEC>(y + r * o.y_stride + c, cols - c, out, log_lanes);
+        if (codes != nullptr) {
+            to_floats<T>(out, t);
+            store_codes<N>(o, t, codes, scales, r, c, pitch - c);
+        }
     }
 }
 
@@ -95,94 +124,130 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(512)
 rmsnorm_forward_long_kernel(const NormRows o, const T* x, const T* res, const T* __restrict__ w, T* sum, T* y, uint8_t* codes, uint8_t* scales, float* rstd)
 {
+    constexpr int N = kPiece<T>;
     __shared__ float part[2][16];
     pdl_release_next_grid();
     const long long r = blockIdx.x;
-    const T *xr = x + r * o.x_stride, *rr = res + (res != nullptr ? r * o.r_stride : 0);
-    T* sr = sum + (sum != nullptr ? r * o.s_stride : 0);
+    const T *xr = x + r * o.x_stride, *rr = res + r * o.r_stride, *x_end = end_of(x, o, o.x_stride), *r_end = end_of(res, o, o.r_stride);
+    T* sr = sum + r * o.s_stride;
     int turn = 0;
     float q = 0.f;
     pdl_wait_prior_grid();
-    for (int c = 8 * threadIdx.x; c < o.cols; c += 4096) {
-        float v[8], t[8];
-        load8<VEC>(xr + c, o.cols - c, v);
-        if (res != nullptr) {
-            load8<VEC>(rr + c, o.cols - c, t);
+    for (int c0 = 0; c0 < o.cols; c0 += 512 * N) {
+        const int c = c0 + N * threadIdx.x;
+        float f[N], t = 0.f;
+        Piece<T, VEC> px, pr;
+        px.start(xr + c, o.cols - c, x_end);
+        if (res != nullptr) pr.start(rr + c, o.cols - c, r_end);
+        uint4 v = px.value(xr + c, o.cols - c, x_end);
+        if (res != nullptr) v = add_pieces<T>(v, pr.value(rr + c, o.cols - c, r_end));
+        if (sum != nullptr) store_piece<T, VEC>(sr + c, o.cols - c, v, 9);
+        to_floats<T>(v, f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = act_type_round<T>(v[j] + t[j]);
-        }
-        if (sum != nullptr) store8<VEC>(sr + c, o.cols - c, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q = fmaf(v[j], v[j], q);
+        for (int j = 0; j < N; ++j) t = fmaf(f[j], f[j], t);
+        q += t;
     }
-    q = team_sum(q, 9, part, turn);
+    q = team_sum(q, 9, part, turn);          // (a barrier: the neighbours' stores of a shared 16 bytes are seen below)
     const float rs = 1.f / sqrtf(q / (float)o.cols + o.eps);
     if (threadIdx.x == 0 && rstd != nullptr) rstd[r] = rs;
-    const T* again = sum != nullptr ? sr : xr;         // (what this thread has written itself)
-    for (int c0 = 0; c0 < o.cols; c0 += 4096) {
-        const int c = c0 + 8 * threadIdx.x;
-        float v[8], t[8];
-        load8<VEC>(again + c, o.cols - c, v);
-        load8<true>(w + c, o.cols - c, t);
+    const T *again = sum != nullptr ? sr : xr, *a_end = sum != nullptr ? end_of(const_cast<const T*>(sum), o, o.s_stride) : x_end;
+    for (int c0 = 0; c0 < o.cols; c0 += 512 * N) {
+        const int c = c0 + N * threadIdx.x;
+        float f[N], t[N];
+        Piece<T, VEC> pv;
+        Piece<T, true> pw;
+        pv.start(again + c, o.cols - c, a_end);
+        pw.start(w + c, o.cols - c, nullptr);
+        to_floats<T>(pv.value(again + c, o.cols - c, a_end), f);
+        to_floats<T>(pw.value(w + c, o.cols - c, nullptr), t);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] = act_type_round<T>(v[j] * rs * t[j]);
-        if (y != nullptr) store8<VEC>(y + r * o.y_stride + c, o.cols - c, t);
-        if (codes != nullptr) store_codes(o, t, codes, scales, r, c, o.pitch - c);
+        for (int j = 0; j < N; ++j) t[j] = f[j] * rs * t[j];
+        const uint4 out = from_floats<T>(t);
+        if (y != nullptr) store_piece<T, VEC>(y + r * o.y_stride + c, o.cols - c, out, 9);
+        if (codes != nullptr) {
+            to_floats<T>(out, t);
+            store_codes<N>(o, t, codes, scales, r, c, o.pitch - c);
+        }
     }
 }
 
 // Backward.  A block stays and its teams take rows in turn; a thread keeps the sums over rows of dy h for its channels, which the
-// teams of a block add up in order at the end: partial[block][cols].
+// teams of a block add up in order at the end: partial[block][cols].  The three tensors of a row are loaded together and kept as they are: the products of the
+// first half are formed again after the mean.
 template <typename T, int NU, bool VEC>
 __global__ void __launch_bounds__(512)
 rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, const T* __restrict__ w, const float* __restrict__ rstd, T* dx, float* __restrict__ partial, int log_lanes)
 {
+    constexpr int N = kPiece<T>;
     extern __shared__ float s_dw[];
     __shared__ float part[2][16];
     pdl_release_next_grid();
     const int lanes = 1 << log_lanes, l = threadIdx.x & (lanes - 1), team = threadIdx.x >> log_lanes, teams = blockDim.x >> log_lanes;
-    float acc[NU][8];
+    const T *dy_end = end_of(dy, o, o.y_stride), *ds_end = end_of(ds, o, o.s_stride), *s_end = end_of(s, o, o.s_stride);
+    float acc[NU][N];
 #pragma unroll
     for (int i = 0; i < NU; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
+        for (int j = 0; j < N; ++j) acc[i][j] = 0.f;
     int turn = 0;
     pdl_wait_prior_grid();
+    uint4 vw[NU];
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+        const int c = N * (i * lanes + l);
+        Piece<T, true> pw;
+        pw.start(w + c, o.cols - c, nullptr);
+        vw[i] = pw.value(w + c, o.cols - c, nullptr);
+    }
+    const float inv = 1.f / (float)o.cols;
     const long long step = (long long)gridDim.x * teams;
     for (long long row = (long long)blockIdx.x * teams + team; row < o.rows; row += step) {
-        float g[NU][8], h[NU][8];
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const int c = 8 * (i * lanes + l);
-            load8<VEC>(dy + row * o.y_stride + c, o.cols - c, g[i]);
-            load8<VEC>(s + row * o.s_stride + c, o.cols - c, h[i]);
-        }
+        uint4 vg[NU], vs[NU], vd[NU];
+        const T *dyr = dy + row * o.y_stride, *sr = s + row * o.s_stride, *dsr = ds + row * o.s_stride;
         const float rs = rstd[row];
+        {
+            Piece<T, VEC> pg[NU], ps[NU], pd[NU];
+#pragma unroll
+            for (int i = 0; i < NU; ++i) {
+                const int c = N * (i * lanes + l);
+                pg[i].start(dyr + c, o.cols - c, dy_end);
+                ps[i].start(sr + c, o.cols - c, s_end);
+            }
+#pragma unroll
+            for (int i = 0; i < NU; ++i) {
+                const int c = N * (i * lanes + l);
+                pd[i].start(dsr + c, ds != nullptr ? o.cols - c : 0, ds_end);
+            }
+#pragma unroll
+            for (int i = 0; i < NU; ++i) {
+                const int c = N * (i * lanes + l);
+                vg[i] = pg[i].value(dyr + c, o.cols - c, dy_end);
+                vs[i] = ps[i].value(sr + c, o.cols - c, s_end);
+                vd[i] = pd[i].value(dsr + c, ds != nullptr ? o.cols - c : 0, ds_end);
+            }
+        }
         float dot = 0.f;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int c = 8 * (i * lanes + l);
-            float t[8];
-            load8<true>(w + c, o.cols - c, t);
+            float g[N], h[N], t[N], sum = 0.f;
+            to_floats<T>(vg[i], g); to_floats<T>(vs[i], h); to_floats<T>(vw[i], t);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                h[i][j] *= rs;
-                acc[i][j] = fmaf(g[i][j], h[i][j], acc[i][j]);
-                g[i][j] *= t[j];
-                dot = fmaf(g[i][j], h[i][j], dot);
+            for (int j = 0; j < N; ++j) {
+                const float gh = g[j] * (h[j] * rs);
+                acc[i][j] += gh;
+                sum = fmaf(gh, t[j], sum);
             }
+            dot += sum;
         }
-        dot = team_sum(dot, log_lanes, part, turn) / (float)o.cols;
+        dot = team_sum(dot, log_lanes, part, turn) * inv;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int c = 8 * (i * lanes + l);
-            float t[8];
+            const int c = N * (i * lanes + l);
+            float g[N], h[N], t[N], d[N];
+            to_floats<T>(vg[i], g); to_floats<T>(vs[i], h); to_floats<T>(vw[i], t); to_floats<T>(vd[i], d);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] = 0.f;
-            if (ds != nullptr) load8<VEC>(ds + row * o.s_stride + c, o.cols - c, t);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] = fmaf(rs, g[i][j] - h[i][j] * dot, t[j]);
-            store8<VEC>(dx + row * o.x_stride + c, o.cols - c, t);
+            for (int j = 0; j < N; ++j) d[j] = fmaf(rs, g[j] * t[j] - h[j] * rs * dot, d[j]);
+            store_piece<T, VEC>(dx + row * o.x_stride + c, o.cols - c, from_floats<T>(d), log_lanes);
         }
     }
     if (partial == nullptr) return;
@@ -191,9 +256,9 @@ rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, 
         if (team == t) {
 #pragma unroll
             for (int i = 0; i < NU; ++i) {
-                const int c = 8 * (i * lanes + l);
+                const int c = N * (i * lanes + l);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
+                for (int j = 0; j < N; ++j) {
                     const float v = t == 0 ? acc[i][j] : s_dw[c + j] + acc[i][j];
                     if (t + 1 < teams) s_dw[c + j] = v;
                     else if (c + j < o.cols) out[c + j] = v;
@@ -208,31 +273,38 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(512)
 rmsnorm_backward_long_kernel(const NormRows o, const T* dy, const T* ds, const T* s, const T* __restrict__ w, const float* __restrict__ rstd, T* dx)
 {
+    constexpr int N = kPiece<T>;
     __shared__ float part[2][16];
     pdl_release_next_grid();
     const long long row = blockIdx.x;
+    const T *dyr = dy + row * o.y_stride, *sr = s + row * o.s_stride, *dsr = ds + row * o.s_stride;
+    const T *dy_end = end_of(dy, o, o.y_stride), *ds_end = end_of(ds, o, o.s_stride), *s_end = end_of(s, o, o.s_stride);
     int turn = 0;
     float dot = 0.f;
     pdl_wait_prior_grid();
     const float rs = rstd[row];
     for (int pass = 0; pass < 2; ++pass) {
-        for (int c = 8 * threadIdx.x; c < o.cols; c += 4096) {
-            float g[8], h[8], t[8];
-            load8<VEC>(dy + row * o.y_stride + c, o.cols - c, g);
-            load8<VEC>(s + row * o.s_stride + c, o.cols - c, h);
-            load8<true>(w + c, o.cols - c, t);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) { g[j] *= t[j]; h[j] *= rs; }
+        for (int c0 = 0; c0 < o.cols; c0 += 512 * N) {
+            const int c = c0 + N * threadIdx.x, d_left = pass == 1 && ds != nullptr ? o.cols - c : 0;
+            float g[N], h[N], t[N], d[N], sum = 0.f;
+            Piece<T, VEC> pg, ps, pd;
+            Piece<T, true> pw;
+            pg.start(dyr + c, o.cols - c, dy_end);
+            ps.start(sr + c, o.cols - c, s_end);
+            pd.start(dsr + c, d_left, ds_end);
+            pw.start(w + c, o.cols - c, nullptr);
+            to_floats<T>(pg.value(dyr + c, o.cols - c, dy_end), g);
+            to_floats<T>(ps.value(sr + c, o.cols - c, s_end), h);
+            to_floats<T>(pd.value(dsr + c, d_left, ds_end), d);
+            to_floats<T>(pw.value(w + c, o.cols - c, nullptr), t);
             if (pass == 0) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dot = fmaf(g[j], h[j], dot);
+                for (int j = 0; j < N; ++j) sum = fmaf(g[j] * t[j], h[j] * rs, sum);
+                dot += sum;
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) t[j] = 0.f;
-                if (ds != nullptr) load8<VEC>(ds + row * o.s_stride + c, o.cols - c, t);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) t[j] = fmaf(rs, g[j] - h[j] * dot, t[j]);
-                store8<VEC>(dx + row * o.x_stride + c, o.cols - c, t);
+                for (int j = 0; j < N; ++j) d[j] = fmaf(rs, g[j] * t[j] - h[j] * rs * dot, d[j]);
+                store_piece<T, VEC>(dx + row * o.x_stride + c, o.cols - c, from_floats<T>(d), 9);
             }
         }
         if (pass == 0) dot = team_sum(dot, 9, part, turn) / (float)o.cols;
@@ -255,42 +327,43 @@ rmsnorm_weight_long_kernel(const NormRows o, const T* dy, const T* s, const floa
 }
 
 // ---------------------------------------------------------------- host side
-constexpr int kMaxCols = 512 * 4 * 8;          // channels that a team's registers hold
-
-struct Team { int log_lanes, nu; };
-// threads of a row: four pieces each, or fewer where that leaves SMs without work
-Team team_of(const NormRows& o)
+struct Team { int log_lanes, nu; };          // nu = 0: a row does not fit a team's registers
+// threads of a row: `most` pieces each, or fewer where that leaves SMs without work
+Team team_of(const NormRows& o, int most)
 {
-    const int units = (o.cols + 7) / 8;
+    const int n = o.bf16 ? 8 : 4, pieces = (o.cols + n - 1) / n;
     Team t{5, 0};
-    while (t.log_lanes < 9 && 4 << t.log_lanes < units) ++t.log_lanes;
-    while (t.log_lanes < 9 && 1 << t.log_lanes < units && o.rows << t.log_lanes < 148 * 512) ++t.log_lanes;
-    const int per = (units + (1 << t.log_lanes) - 1) >> t.log_lanes;
-    t.nu = per <= 1 ? 1 : per <= 2 ? 2 : 4;
+    while (t.log_lanes < 9 && most << t.log_lanes < pieces) ++t.log_lanes;
+    while (t.log_lanes < 9 && 1 << t.log_lanes < pieces && o.rows << t.log_lanes < 148 * 512) ++t.log_lanes;
+    const int per = (pieces + (1 << t.log_lanes) - 1) >> t.log_lanes;
+    t.nu = per <= 1 ? 1 : per <= 2 ? 2 : per <= 4 && most == 4 ? 4 : 0;
     return t;
 }
-bool vectors(const NormRows& o, int elem, long long a, long long b, long long c, long long d)
+bool vectors(const NormRows& o, long long a, long long b, long long c, long long d)
 {
-    const int n = 16 / elem;
+    const int n = o.bf16 ? 8 : 4;
     return a % n == 0 && b % n == 0 && c % n == 0 && d % n == 0;
 }
-int backward_blocks(const NormRows& o, const Team& t, int threads)
-{
-    const long long teams = threads >> t.log_lanes, need = (o.rows + teams - 1) / teams;
-    return (int)std::min<long long>(need, device_sms() * (1024 / threads));
-}
 constexpr int kBackwardThreads = 512;
+// (pieces on any boundary take twice the registers on their way)
+bool backward_vectors(const NormRows& o) { return vectors(o, o.y_stride, o.s_stride, o.x_stride, 0); }
+Team backward_team(const NormRows& o) { return team_of(o, backward_vectors(o) ? 4 : 2); }
+int backward_blocks(const NormRows& o, const Team& t)
+{
+    const long long teams = kBackwardThreads >> t.log_lanes, need = (o.rows + teams - 1) / teams;
+    return (int)std::min<long long>(need, device_sms());
+}
 
 template <typename T>
 cudaError_t forward(const NormRows& o, const T* x, const T* res, const T* w, T* sum, T* y, uint8_t* codes, uint8_t* scales, float* rstd, cudaStream_t stream)
 {
-    const bool vec = vectors(o, sizeof(T), o.x_stride, res ? o.r_stride : 0, sum ? o.s_stride : 0, y ? o.y_stride : 0);
+    const bool vec = vectors(o, o.x_stride, res ? o.r_stride : 0, sum ? o.s_stride : 0, y ? o.y_stride : 0);
+    const Team t = team_of(o, 4);
     note_launch();
-    if (o.cols > kMaxCols) {
+    if (t.nu == 0) {
         auto kern = vec ? rmsnorm_forward_long_kernel<T, true> : rmsnorm_forward_long_kernel<T, false>;
         return launch_kernel(kern, dim3((unsigned)o.rows), dim3(512), 0, stream, dim3(1, 1, 1), o, x, res, w, sum, y, codes, scales, rstd);
     }
-    const Team t = team_of(o);
     const int threads = std::max(128, 1 << t.log_lanes), teams = threads >> t.log_lanes;
     auto kern = t.nu == 1 ? (vec ? rmsnorm_forward_kernel<T, 1, true> : rmsnorm_forward_kernel<T, 1, false>)
               : t.nu == 2 ? (vec ? rmsnorm_forward_kernel<T, 2, true> : rmsnorm_forward_kernel<T, 2, false>)
@@ -301,13 +374,13 @@ cudaError_t forward(const NormRows& o, const T* x, const T* res, const T* w, T* 
 template <typename T>
 cudaError_t backward(const NormRows& o, const T* dy, const T* ds, const T* s, const T* w, const float* rstd, T* dx, float* dweight, float* partial, cudaStream_t stream)
 {
-    const bool vec = vectors(o, sizeof(T), o.y_stride, o.s_stride, o.x_stride, 0);
+    const bool vec = backward_vectors(o);
+    const Team t = backward_team(o);
     cudaError_t err;
-    int splits;
+    const int splits = norm_partials(o);
     note_launch();
-    if (o.cols > kMaxCols) {
+    if (t.nu == 0) {
         if (dweight != nullptr) {
-            splits = norm_partials(o);
             err = launch_kernel(rmsnorm_weight_long_kernel<T>, dim3((unsigned)((o.cols + 255) / 256), (unsigned)splits), dim3(256), 0, stream, dim3(1, 1, 1), o, dy, s, rstd, partial);
             if (err != cudaSuccess) return err;
             note_launch();
@@ -315,12 +388,10 @@ cudaError_t backward(const NormRows& o, const T* dy, const T* ds, const T* s, co
         auto kern = vec ? rmsnorm_backward_long_kernel<T, true> : rmsnorm_backward_long_kernel<T, false>;
         err = launch_kernel(kern, dim3((unsigned)o.rows), dim3(512), 0, stream, dim3(1, 1, 1), o, dy, ds, s, w, rstd, dx);
     } else {
-        const Team t = team_of(o);
-        splits = backward_blocks(o, t, kBackwardThreads);
         auto kern = t.nu == 1 ? (vec ? rmsnorm_backward_kernel<T, 1, true> : rmsnorm_backward_kernel<T, 1, false>)
                   : t.nu == 2 ? (vec ? rmsnorm_backward_kernel<T, 2, true> : rmsnorm_backward_kernel<T, 2, false>)
-                              : (vec ? rmsnorm_backward_kernel<T, 4, true> : rmsnorm_backward_kernel<T, 4, false>);
-        const size_t smem = kBackwardThreads >> t.log_lanes > 1 ? (size_t)t.nu * 32 << t.log_lanes : 0;      // (at most 32 KB)
+                              : rmsnorm_backward_kernel<T, 4, true>;
+        const size_t smem = kBackwardThreads >> t.log_lanes > 1 ? (size_t)t.nu * kPiece<T> * 4 << t.log_lanes : 0;      // (at most 32 KB)
         err = launch_kernel(kern, dim3((unsigned)splits), dim3(kBackwardThreads), smem, stream, dim3(1, 1, 1), o, dy, ds, s, w, rstd, dx, dweight != nullptr ? partial : nullptr, t.log_lanes);
     }
     if (err != cudaSuccess || dweight == nullptr) return err;
@@ -333,7 +404,8 @@ cudaError_t backward(const NormRows& o, const T* dy, const T* ds, const T* s, co
 int norm_partials(const NormRows& o)
 {
     if (o.rows == 0) return 0;
-    if (o.cols <= kMaxCols) return backward_blocks(o, team_of(o), kBackwardThreads);
+    const Team t = backward_team(o);
+    if (t.nu != 0) return backward_blocks(o, t);
     return (int)std::min<long long>((o.rows + 31) / 32, 64);
 }
 
