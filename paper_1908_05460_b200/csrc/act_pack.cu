@@ -18,7 +18,7 @@ struct RowsOp {
     int log_lanes;              // threads of a row
 };
 
-template <typename T, int FMT, bool VEC>
+template <typename T, int FMT, bool FULL>
 __global__ void __launch_bounds__(kBlock)
 act_pack_kernel(const T* x, uint8_t* codes, uint8_t* scales, const RowsOp o)
 {
@@ -26,31 +26,31 @@ act_pack_kernel(const T* x, uint8_t* codes, uint8_t* scales, const RowsOp o)
     pdl_release_next_grid();
     const int lanes = 1 << o.log_lanes, l = threadIdx.x & (lanes - 1);
     const long long row = (long long)blockIdx.x * (kBlock >> o.log_lanes) + (threadIdx.x >> o.log_lanes), r = row < o.rows ? row : 0;
-    const int cols = row < o.rows ? o.cols : 0, pitch = row < o.rows ? o.pitch : 0;
-    const T *src = x + r * o.stride, *end = x + (o.rows - 1) * o.stride + o.cols;
+    const int pitch = row < o.rows ? o.pitch : 0;
+    const Row<T, FULL> src(x, r, o.stride, o.rows, o.cols, row < o.rows);
     uint8_t* dst = codes + r * o.pitch;
     uint8_t* sc = scales + r * o.groups;
     pdl_wait_prior_grid();
     const int pieces = 32 / N * o.groups;         // (every lane of a warp walks as often: shuffles are warp-wide)
     for (int u0 = 0; u0 < pieces; u0 += kAhead * lanes) {
-        Piece<T, VEC> p[kAhead];
+        Piece<T, FULL> p[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const int c = (u0 + i * lanes + l) * N;
-            p[i].start(src + c, cols - c, end);
+            p[i].start(src, c);
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const int c = (u0 + i * lanes + l) * N;
             if (u0 + i * lanes >= pieces) break;
             float v[N];
-            to_floats<T>(p[i].value(src + c, cols - c, end), v);
+            to_floats<T>(p[i].value(src, c), v);
             act_store<FMT, N>(v, dst + c, pitch - c, sc + (c >> 5), (c & 31) == 0);
         }
     }
 }
 
-template <typename T, int FMT, bool VEC>
+template <typename T, int FMT, bool FULL>
 __global__ void __launch_bounds__(kBlock)
 act_unpack_kernel(const uint8_t* codes, const uint8_t* scales, T* x, const RowsOp o)
 {
@@ -97,7 +97,7 @@ act_unpack_kernel(const uint8_t* codes, const uint8_t* scales, T* x, const RowsO
             uint4 v;
             if constexpr (N == 8) v = make_uint4(w[0], w[1], w[2], w[3]);
             else v = make_uint4(w[0] << 16, w[0] & 0xffff0000u, w[1] << 16, w[1] & 0xffff0000u);
-            store_piece<T, VEC>(dst + c, cols - c, v, o.log_lanes);
+            store_piece<T, FULL>(dst + c, cols - c, v, o.log_lanes);
         }
     }
 }
@@ -117,13 +117,13 @@ unsigned row_blocks(const RowsOp& o) { return (unsigned)((o.rows + (kBlock >> o.
 template <typename T, int FMT>
 cudaError_t pack(const T* x, uint8_t* codes, uint8_t* scales, const RowsOp& o, cudaStream_t stream)
 {
-    auto kern = o.stride % kPiece<T> == 0 ? act_pack_kernel<T, FMT, true> : act_pack_kernel<T, FMT, false>;
+    auto kern = o.stride % kPiece<T> == 0 && o.cols % kPiece<T> == 0 ? act_pack_kernel<T, FMT, true> : act_pack_kernel<T, FMT, false>;
     return launch_kernel(kern, dim3(row_blocks(o)), dim3(kBlock), 0, stream, dim3(1, 1, 1), x, codes, scales, o);
 }
 template <typename T, int FMT>
 cudaError_t unpack(const uint8_t* codes, const uint8_t* scales, T* x, const RowsOp& o, cudaStream_t stream)
 {
-    auto kern = o.stride % kPiece<T> == 0 ? act_unpack_kernel<T, FMT, true> : act_unpack_kernel<T, FMT, false>;
+    auto kern = o.stride % kPiece<T> == 0 && o.cols % kPiece<T> == 0 ? act_unpack_kernel<T, FMT, true> : act_unpack_kernel<T, FMT, false>;
     return launch_kernel(kern, dim3(row_blocks(o)), dim3(kBlock), 0, stream, dim3(1, 1, 1), codes, scales, x, o);
 }
 

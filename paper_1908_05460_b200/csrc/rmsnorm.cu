@@ -3,8 +3,8 @@
 //   forward    s = x + r (rounded to the type),  rstd = 1 / sqrt(mean(s^2) + eps),  y = s rstd w (rounded once),  codes, scales = y in 8 bits (act8.cuh)
 //   backward   h = s rstd,  g = dy w,  dx = ds + rstd (g - h mean(g h)),  dw = sum over rows of dy h
 //
-// Bound by HBM: every tensor is read and written once.  A team of `lanes` threads holds a row in registers, `NU` pieces of 16 bytes (rows.cuh) a
-// thread, so that the second use of a row (after its mean) reads nothing.  Sums and means are fp32, in an order that depends on the sizes alone.
+// Bound by HBM: every tensor is read and written once.  A team of `lanes` threads holds a row in registers, `NU` pieces of 16 bytes a thread, by
+// columns where rows are whole pieces (FULL) and by their frame elsewhere (rows.cuh), so that the second use of a row (after its mean) reads nothing.  Sums and means are fp32, in an order that depends on the sizes alone.
 #include <algorithm>
 #include <type_traits>
 
@@ -49,43 +49,56 @@ __device__ __forceinline__ uint4 add_pieces(const uint4& x, const uint4& r)
     for (int j = 0; j < kPiece<T>; ++j) a[j] += b[j];
     return from_floats<T>(a);
 }
-template <typename T>
-__device__ __forceinline__ const T* end_of(const T* p, const NormRows& o, long long stride) { return p + (o.rows - 1) * stride + o.cols; }
+// N elements of the weight from column c on, zeros outside [0, cols)
+template <typename T, bool FULL>
+__device__ __forceinline__ uint4 load_weight(const T* __restrict__ w, int c, int cols)
+{
+    if (FULL) return c < cols ? *reinterpret_cast<const uint4*>(w + c) : make_uint4(0, 0, 0, 0);
+    if (c >= 0) {
+        const Row<T, false> from(w + c, 0, 0, 1, cols - c, c < cols);
+        Piece<T, false> p;
+        p.start(from, 0);
+        return p.value(from, 0);
+    }
+    return shifted16(make_uint4(0, 0, 0, 0), load_slowly(w, min(cols, kPiece<T> + c)), 16 + c * (int)sizeof(T));
+}
 
-template <typename T, int NU, bool VEC>
+template <typename T, int NU, bool FULL>
 __global__ void __launch_bounds__(512)
 rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __restrict__ w, T* sum, T* y, uint8_t* codes, uint8_t* scales, float* rstd, int log_lanes)
 {
     constexpr int N = kPiece<T>;
     __shared__ float part[2][16];
+    __shared__ uint4 s_head[FULL ? 1 : NU + 1][16];
     pdl_release_next_grid();
-    const int lanes = 1 << log_lanes, l = threadIdx.x & (lanes - 1);
+    const int lanes = 1 << log_lanes, l = threadIdx.x & (lanes - 1), warp = threadIdx.x >> 5;
     const long long row = (long long)blockIdx.x * (blockDim.x >> log_lanes) + (threadIdx.x >> log_lanes);
     const bool live = row < o.rows;          // (teams without a row go along: shuffles and barriers are shared)
     const long long r = live ? row : 0;
     const int cols = live ? o.cols : 0;
-    const T *xr = x + r * o.x_stride, *rr = res + r * o.r_stride, *x_end = end_of(x, o, o.x_stride), *r_end = end_of(res, o, o.r_stride);
+    const Row<T, FULL> rx(x, r, o.x_stride, o.rows, o.cols, live), rr(res, r, o.r_stride, o.rows, o.cols, live);
+    const int shift = FULL ? 0 : rx.off / (int)sizeof(T);          // the frame: columns -shift, N - shift, ...
     int turn = 0;
     pdl_wait_prior_grid();
     uint4 v[NU];
     {
-        Piece<T, VEC> px[NU], pr[NU];
+        FramePiece<T, FULL> px[NU], pr[NU];
 #pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const int c = N * (i * lanes + l);
-            px[i].start(xr + c, cols - c, x_end);
-            if (res != nullptr) pr[i].start(rr + c, cols - c, r_end);
+        for (int i = 0; i < NU; ++i) px[i].start(rx, N * (i * lanes + l) - shift);
+        if (res != nullptr) {
+#pragma unroll
+            for (int i = 0; i < NU; ++i) pr[i].start(rr, N * (i * lanes + l) - shift);
         }
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int c = N * (i * lanes + l);
-            v[i] = px[i].value(xr + c, cols - c, x_end);
-            if (res != nullptr) v[i] = add_pieces<T>(v[i], pr[i].value(rr + c, cols - c, r_end));
+            const int c = N * (i * lanes + l) - shift;
+            v[i] = px[i].value(rx, c);
+            if (res != nullptr) v[i] = add_pieces<T>(v[i], pr[i].value(rr, c));
         }
     }
     if (sum != nullptr) {
 #pragma unroll
-        for (int i = 0; i < NU; ++i) store_piece<T, VEC>(sum + r * o.s_stride + N * (i * lanes + l), cols - N * (i * lanes + l), v[i], log_lanes);
+        for (int i = 0; i < NU; ++i) store_frame<T, FULL>(sum + r * o.s_stride, N * (i * lanes + l) - shift, cols, v[i]);
     }
     float q = 0.f;
 #pragma unroll
@@ -95,32 +108,50 @@ rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __re
 #pragma unroll
         for (int j = 0; j < N; ++j) t = fmaf(f[j], f[j], t);
         q += t;
+        if (!FULL && (l & 31) == 0) s_head[i][warp] = v[i];
     }
-    q = team_sum(q, log_lanes, part, turn);
+    if (!FULL) {
+        if (l == 0) s_head[NU][warp] = make_uint4(0, 0, 0, 0);
+        __syncwarp();
+    }
+    q = team_sum(q, log_lanes, part, turn);          // (and a barrier of the team, where it has several warps)
     const float rs = 1.f / sqrtf(q / (float)o.cols + o.eps);
     if (live && l == 0 && rstd != nullptr) rstd[r] = rs;
     const int pitch = live ? o.pitch : 0;
+    auto output = [&](const uint4& s, int c) {
+        float f[N], t[N];
+        to_floats<T>(load_weight<T, FULL>(w, c, o.cols), t);
+        to_floats<T>(s, f);
+#pragma unroll
+        for (int j = 0; j < N; ++j) t[j] = f[j] * rs * t[j];
+        return from_floats<T>(t);
+    };
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
         const int c = N * (i * lanes + l);
-        float f[N], t[N];
-        Piece<T, true> pw;
-        pw.start(w + c, o.cols - c, nullptr);
-        to_floats<T>(pw.value(w + c, o.cols - c, nullptr), t);
-        to_floats<T>(v[i], f);
-#pragma unroll
-        for (int j = 0; j < N; ++j) t[j] = f[j] * rs * t[j];
-        const uint4 out = from_floats<T>(t);
-        if (y != nullptr) store_piece<T, VEC>(y + r * o.y_stride + c, cols - c, out, log_lanes);
+        uint4 out = output(v[i], c - shift);
+        if (y != nullptr) store_frame<T, FULL>(y + r * o.y_stride, c - shift, cols, out);
         if (codes != nullptr) {
+            if (!FULL) {        // from the frame to columns: with what the next piece of the frame has, a lane up or, for a warp's last lane, of its neighbour's first
+                uint4 next;
+                next.x = __shfl_down_sync(0xffffffffu, out.x, 1); next.y = __shfl_down_sync(0xffffffffu, out.y, 1);
+                next.z = __shfl_down_sync(0xffffffffu, out.z, 1); next.w = __shfl_down_sync(0xffffffffu, out.w, 1);
+                if ((l & 31) == 31) {
+                    const bool wraps = l == lanes - 1;
+                    next = output(s_head[wraps ? i + 1 : i][wraps ? warp - (lanes >> 5) + 1 : warp + 1], c - shift + N);
+                }
+                out = shifted16(out, next, shift * (int)sizeof(T));
+            }
+            float t[N];
             to_floats<T>(out, t);
             store_codes<N>(o, t, codes, scales, r, c, pitch - c);
         }
     }
 }
 
-// Rows longer than a team's registers: a block a row, which it reads twice (the second time from L2 or, of very long rows, from memory).
-template <typename T, bool VEC>
+// Rows longer than a team's registers, or tensors whose rows lie on different boundaries: a block a row, which it reads twice (the second time from
+// L2 or, of very long rows, from memory), by columns.
+template <typename T, bool FULL>
 __global__ void __launch_bounds__(512)
 rmsnorm_forward_long_kernel(const NormRows o, const T* x, const T* res, const T* __restrict__ w, T* sum, T* y, uint8_t* codes, uint8_t* scales, float* rstd)
 {
@@ -128,7 +159,7 @@ rmsnorm_forward_long_kernel(const NormRows o, const T* x, const T* res, const T*
     __shared__ float part[2][16];
     pdl_release_next_grid();
     const long long r = blockIdx.x;
-    const T *xr = x + r * o.x_stride, *rr = res + r * o.r_stride, *x_end = end_of(x, o, o.x_stride), *r_end = end_of(res, o, o.r_stride);
+    const Row<T, FULL> rx(x, r, o.x_stride, o.rows, o.cols, true), rr(res, r, o.r_stride, o.rows, o.cols, true);
     T* sr = sum + r * o.s_stride;
     int turn = 0;
     float q = 0.f;
@@ -136,12 +167,12 @@ rmsnorm_forward_long_kernel(const NormRows o, const T* x, const T* res, const T*
     for (int c0 = 0; c0 < o.cols; c0 += 512 * N) {
         const int c = c0 + N * threadIdx.x;
         float f[N], t = 0.f;
-        Piece<T, VEC> px, pr;
-        px.start(xr + c, o.cols - c, x_end);
-        if (res != nullptr) pr.start(rr + c, o.cols - c, r_end);
-        uint4 v = px.value(xr + c, o.cols - c, x_end);
-        if (res != nullptr) v = add_pieces<T>(v, pr.value(rr + c, o.cols - c, r_end));
-        if (sum != nullptr) store_piece<T, VEC>(sr + c, o.cols - c, v, 9);
+        Piece<T, FULL> px, pr;
+        px.start(rx, c);
+        pr.start(rr, c);
+        uint4 v = px.value(rx, c);
+        if (res != nullptr) v = add_pieces<T>(v, pr.value(rr, c));
+        if (sum != nullptr) store_piece<T, FULL>(sr + c, o.cols - c, v, 9);
         to_floats<T>(v, f);
 #pragma unroll
         for (int j = 0; j < N; ++j) t = fmaf(f[j], f[j], t);
@@ -150,20 +181,18 @@ rmsnorm_forward_long_kernel(const NormRows o, const T* x, const T* res, const T*
     q = team_sum(q, 9, part, turn);          // (a barrier: the neighbours' stores of a shared 16 bytes are seen below)
     const float rs = 1.f / sqrtf(q / (float)o.cols + o.eps);
     if (threadIdx.x == 0 && rstd != nullptr) rstd[r] = rs;
-    const T *again = sum != nullptr ? sr : xr, *a_end = sum != nullptr ? end_of(const_cast<const T*>(sum), o, o.s_stride) : x_end;
+    const Row<T, FULL> again(sum != nullptr ? sum : x, r, sum != nullptr ? o.s_stride : o.x_stride, o.rows, o.cols, true);
     for (int c0 = 0; c0 < o.cols; c0 += 512 * N) {
         const int c = c0 + N * threadIdx.x;
         float f[N], t[N];
-        Piece<T, VEC> pv;
-        Piece<T, true> pw;
-        pv.start(again + c, o.cols - c, a_end);
-        pw.start(w + c, o.cols - c, nullptr);
-        to_floats<T>(pv.value(again + c, o.cols - c, a_end), f);
-        to_floats<T>(pw.value(w + c, o.cols - c, nullptr), t);
+        Piece<T, FULL> pv;
+        pv.start(again, c);
+        to_floats<T>(load_weight<T, FULL>(w, c, o.cols), t);
+        to_floats<T>(pv.value(again, c), f);
 #pragma unroll
         for (int j = 0; j < N; ++j) t[j] = f[j] * rs * t[j];
         const uint4 out = from_floats<T>(t);
-        if (y != nullptr) store_piece<T, VEC>(y + r * o.y_stride + c, o.cols - c, out, 9);
+        if (y != nullptr) store_piece<T, FULL>(y + r * o.y_stride + c, o.cols - c, out, 9);
         if (codes != nullptr) {
             to_floats<T>(out, t);
             store_codes<N>(o, t, codes, scales, r, c, o.pitch - c);
@@ -172,9 +201,10 @@ rmsnorm_forward_long_kernel(const NormRows o, const T* x, const T* res, const T*
 }
 
 // Backward.  A block stays and its teams take rows in turn; a thread keeps the sums over rows of dy h for its channels, which the
-// teams of a block add up in order at the end: partial[block][cols].  The three tensors of a row are loaded together and kept as they are: the products of the
-// first half are formed again after the mean.
-template <typename T, int NU, bool VEC>
+// teams of a block add up in order at the end: partial[block][cols].  A team's rows are a multiple of N apart, so that they have one frame, and a thread the
+// same channels in each.  The three tensors of a row are loaded while the row before is worked on, and kept as they are: the products of the first half are
+// formed again after the mean.
+template <typename T, int NU, bool FULL>
 __global__ void __launch_bounds__(512)
 rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, const T* __restrict__ w, const float* __restrict__ rstd, T* dx, float* __restrict__ partial, int log_lanes)
 {
@@ -183,49 +213,45 @@ rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, 
     __shared__ float part[2][16];
     pdl_release_next_grid();
     const int lanes = 1 << log_lanes, l = threadIdx.x & (lanes - 1), team = threadIdx.x >> log_lanes, teams = blockDim.x >> log_lanes;
-    const T *dy_end = end_of(dy, o, o.y_stride), *ds_end = end_of(ds, o, o.s_stride), *s_end = end_of(s, o, o.s_stride);
     float acc[NU][N];
 #pragma unroll
     for (int i = 0; i < NU; ++i)
 #pragma unroll
         for (int j = 0; j < N; ++j) acc[i][j] = 0.f;
     int turn = 0;
+    const long long step = (long long)gridDim.x * teams;
+    long long row = (long long)blockIdx.x * teams + team;
+    const int shift = FULL ? 0 : (int)((row * o.s_stride) % N);
     pdl_wait_prior_grid();
     uint4 vw[NU];
 #pragma unroll
-    for (int i = 0; i < NU; ++i) {
-        const int c = N * (i * lanes + l);
-        Piece<T, true> pw;
-        pw.start(w + c, o.cols - c, nullptr);
-        vw[i] = pw.value(w + c, o.cols - c, nullptr);
-    }
+    for (int i = 0; i < NU; ++i) vw[i] = load_weight<T, FULL>(w, N * (i * lanes + l) - shift, o.cols);
     const float inv = 1.f / (float)o.cols;
-    const long long step = (long long)gridDim.x * teams;
-    for (long long row = (long long)blockIdx.x * teams + team; row < o.rows; row += step) {
+    FramePiece<T, FULL> pg[NU], ps[NU], pd[NU];
+    float rs_next = 0.f;
+    auto start = [&](long long row) {
+        const bool live = row < o.rows;
+        const Row<T, FULL> rg(dy, row, o.y_stride, o.rows, o.cols, live), rh(s, row, o.s_stride, o.rows, o.cols, live), rd(ds, row, o.s_stride, o.rows, o.cols, live);
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+            const int c = N * (i * lanes + l) - shift;
+            pg[i].start(rg, c); ps[i].start(rh, c); pd[i].start(rd, c);
+        }
+        if (live) rs_next = __ldg(rstd + row);
+    };
+    start(row);
+    for (; row < o.rows; row += step) {
         uint4 vg[NU], vs[NU], vd[NU];
-        const T *dyr = dy + row * o.y_stride, *sr = s + row * o.s_stride, *dsr = ds + row * o.s_stride;
-        const float rs = rstd[row];
+        const float rs = rs_next;
         {
-            Piece<T, VEC> pg[NU], ps[NU], pd[NU];
+            const Row<T, FULL> rg(dy, row, o.y_stride, o.rows, o.cols, true), rh(s, row, o.s_stride, o.rows, o.cols, true), rd(ds, row, o.s_stride, o.rows, o.cols, true);
 #pragma unroll
             for (int i = 0; i < NU; ++i) {
-                const int c = N * (i * lanes + l);
-                pg[i].start(dyr + c, o.cols - c, dy_end);
-                ps[i].start(sr + c, o.cols - c, s_end);
-            }
-#pragma unroll
-            for (int i = 0; i < NU; ++i) {
-                const int c = N * (i * lanes + l);
-                pd[i].start(dsr + c, ds != nullptr ? o.cols - c : 0, ds_end);
-            }
-#pragma unroll
-            for (int i = 0; i < NU; ++i) {
-                const int c = N * (i * lanes + l);
-                vg[i] = pg[i].value(dyr + c, o.cols - c, dy_end);
-                vs[i] = ps[i].value(sr + c, o.cols - c, s_end);
-                vd[i] = pd[i].value(dsr + c, ds != nullptr ? o.cols - c : 0, ds_end);
+                const int c = N * (i * lanes + l) - shift;
+                vg[i] = pg[i].value(rg, c); vs[i] = ps[i].value(rh, c); vd[i] = pd[i].value(rd, c);
             }
         }
+        start(row + step);
         float dot = 0.f;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
@@ -242,12 +268,11 @@ rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, 
         dot = team_sum(dot, log_lanes, part, turn) * inv;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int c = N * (i * lanes + l);
             float g[N], h[N], t[N], d[N];
             to_floats<T>(vg[i], g); to_floats<T>(vs[i], h); to_floats<T>(vw[i], t); to_floats<T>(vd[i], d);
 #pragma unroll
             for (int j = 0; j < N; ++j) d[j] = fmaf(rs, g[j] * t[j] - h[j] * rs * dot, d[j]);
-            store_piece<T, VEC>(dx + row * o.x_stride + c, o.cols - c, from_floats<T>(d), log_lanes);
+            store_frame<T, FULL>(dx + row * o.x_stride, N * (i * lanes + l) - shift, o.cols, from_floats<T>(d));
         }
     }
     if (partial == nullptr) return;
@@ -256,12 +281,12 @@ rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, 
         if (team == t) {
 #pragma unroll
             for (int i = 0; i < NU; ++i) {
-                const int c = N * (i * lanes + l);
+                const int c = N * (i * lanes + l) - shift;
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
+                    if (c + j < 0 || c + j >= o.cols) continue;
                     const float v = t == 0 ? acc[i][j] : s_dw[c + j] + acc[i][j];
-                    if (t + 1 < teams) s_dw[c + j] = v;
-                    else if (c + j < o.cols) out[c + j] = v;
+                    (t + 1 < teams ? s_dw : out)[c + j] = v;
                 }
             }
         }
@@ -269,7 +294,7 @@ rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, 
     }
 }
 
-template <typename T, bool VEC>
+template <typename T, bool FULL>
 __global__ void __launch_bounds__(512)
 rmsnorm_backward_long_kernel(const NormRows o, const T* dy, const T* ds, const T* s, const T* __restrict__ w, const float* __restrict__ rstd, T* dx)
 {
@@ -277,34 +302,31 @@ rmsnorm_backward_long_kernel(const NormRows o, const T* dy, const T* ds, const T
     __shared__ float part[2][16];
     pdl_release_next_grid();
     const long long row = blockIdx.x;
-    const T *dyr = dy + row * o.y_stride, *sr = s + row * o.s_stride, *dsr = ds + row * o.s_stride;
-    const T *dy_end = end_of(dy, o, o.y_stride), *ds_end = end_of(ds, o, o.s_stride), *s_end = end_of(s, o, o.s_stride);
+    const Row<T, FULL> rg(dy, row, o.y_stride, o.rows, o.cols, true), rh(s, row, o.s_stride, o.rows, o.cols, true), rd(ds, row, o.s_stride, o.rows, o.cols, true);
     int turn = 0;
     float dot = 0.f;
     pdl_wait_prior_grid();
     const float rs = rstd[row];
     for (int pass = 0; pass < 2; ++pass) {
         for (int c0 = 0; c0 < o.cols; c0 += 512 * N) {
-            const int c = c0 + N * threadIdx.x, d_left = pass == 1 && ds != nullptr ? o.cols - c : 0;
+            const int c = c0 + N * threadIdx.x;
             float g[N], h[N], t[N], d[N], sum = 0.f;
-            Piece<T, VEC> pg, ps, pd;
-            Piece<T, true> pw;
-            pg.start(dyr + c, o.cols - c, dy_end);
-            ps.start(sr + c, o.cols - c, s_end);
-            pd.start(dsr + c, d_left, ds_end);
-            pw.start(w + c, o.cols - c, nullptr);
-            to_floats<T>(pg.value(dyr + c, o.cols - c, dy_end), g);
-            to_floats<T>(ps.value(sr + c, o.cols - c, s_end), h);
-            to_floats<T>(pd.value(dsr + c, d_left, ds_end), d);
-            to_floats<T>(pw.value(w + c, o.cols - c, nullptr), t);
+            Piece<T, FULL> pg, ps, pd;
+            pg.start(rg, c);
+            ps.start(rh, c);
+            if (pass == 1) pd.start(rd, c);
+            to_floats<T>(load_weight<T, FULL>(w, c, o.cols), t);
+            to_floats<T>(pg.value(rg, c), g);
+            to_floats<T>(ps.value(rh, c), h);
             if (pass == 0) {
 #pragma unroll
                 for (int j = 0; j < N; ++j) sum = fmaf(g[j] * t[j], h[j] * rs, sum);
                 dot += sum;
             } else {
+                to_floats<T>(pd.value(rd, c), d);
 #pragma unroll
                 for (int j = 0; j < N; ++j) d[j] = fmaf(rs, g[j] * t[j] - h[j] * rs * dot, d[j]);
-                store_piece<T, VEC>(dx + row * o.x_stride + c, o.cols - c, from_floats<T>(d), 9);
+                store_piece<T, FULL>(dx + row * o.x_stride + c, o.cols - c, from_floats<T>(d), 9);
             }
         }
         if (pass == 0) dot = team_sum(dot, 9, part, turn) / (float)o.cols;
@@ -327,38 +349,35 @@ rmsnorm_weight_long_kernel(const NormRows o, const T* dy, const T* s, const floa
 }
 
 // ---------------------------------------------------------------- host side
-struct Team { int log_lanes, nu; };          // nu = 0: a row does not fit a team's registers
-// threads of a row: `most` pieces each, or fewer where that leaves SMs without work
-Team team_of(const NormRows& o, int most)
+struct Team { int log_lanes, nu; bool full; };          // nu = 0: a row by blocks, twice
+// threads of a row: `most` pieces each, or fewer where that leaves SMs without work.  strides: of the tensors in the call.
+Team team_of(const NormRows& o, int most, long long a, long long b, long long c, long long d)
 {
-    const int n = o.bf16 ? 8 : 4, pieces = (o.cols + n - 1) / n;
-    Team t{5, 0};
+    const int n = o.bf16 ? 8 : 4;
+    Team t{5, 0, o.cols % n == 0 && a % n == 0 && b % n == 0 && c % n == 0 && d % n == 0};
+    const int pieces = t.full ? o.cols / n : (o.cols + 2 * n - 2) / n;         // (a frame starts up to n - 1 elements early)
     while (t.log_lanes < 9 && most << t.log_lanes < pieces) ++t.log_lanes;
     while (t.log_lanes < 9 && 1 << t.log_lanes < pieces && o.rows << t.log_lanes < 148 * 512) ++t.log_lanes;
     const int per = (pieces + (1 << t.log_lanes) - 1) >> t.log_lanes;
-    t.nu = per <= 1 ? 1 : per <= 2 ? 2 : per <= 4 && most == 4 ? 4 : 0;
+    if (t.full || (a % n == b % n && a % n == c % n && a % n == d % n)) t.nu = per <= 1 ? 1 : per <= 2 ? 2 : per <= 4 && most == 4 ? 4 : 0;
     return t;
 }
-bool vectors(const NormRows& o, long long a, long long b, long long c, long long d)
-{
-    const int n = o.bf16 ? 8 : 4;
-    return a % n == 0 && b % n == 0 && c % n == 0 && d % n == 0;
-}
 constexpr int kBackwardThreads = 512;
-// (pieces on any boundary take twice the registers on their way)
-bool backward_vectors(const NormRows& o) { return vectors(o, o.y_stride, o.s_stride, o.x_stride, 0); }
-Team backward_team(const NormRows& o) { return team_of(o, backward_vectors(o) ? 4 : 2); }
+Team backward_team(const NormRows& o) { return team_of(o, 2, o.y_stride, o.s_stride, o.x_stride, o.s_stride); }
 int backward_blocks(const NormRows& o, const Team& t)
 {
-    const long long teams = kBackwardThreads >> t.log_lanes, need = (o.rows + teams - 1) / teams;
-    return (int)std::min<long long>(need, device_sms());
+    const int teams = kBackwardThreads >> t.log_lanes, n = o.bf16 ? 8 : 4;
+    const long long need = (o.rows + teams - 1) / teams;
+    int most = device_sms();
+    while (!t.full && most > 1 && (long long)most * teams * o.s_stride % n != 0) --most;         // (a team's rows have one frame)
+    return (int)std::min<long long>(need, most);
 }
 
 template <typename T>
 cudaError_t forward(const NormRows& o, const T* x, const T* res, const T* w, T* sum, T* y, uint8_t* codes, uint8_t* scales, float* rstd, cudaStream_t stream)
 {
-    const bool vec = vectors(o, o.x_stride, res ? o.r_stride : 0, sum ? o.s_stride : 0, y ? o.y_stride : 0);
-    const Team t = team_of(o, 4);
+    const Team t = team_of(o, 4, o.x_stride, res ? o.r_stride : o.x_stride, sum ? o.s_stride : o.x_stride, y ? o.y_stride : o.x_stride);
+    const bool vec = t.full;
     note_launch();
     if (t.nu == 0) {
         auto kern = vec ? rmsnorm_forward_long_kernel<T, true> : rmsnorm_forward_long_kernel<T, false>;
@@ -374,8 +393,8 @@ cudaError_t forward(const NormRows& o, const T* x, const T* res, const T* w, T* 
 template <typename T>
 cudaError_t backward(const NormRows& o, const T* dy, const T* ds, const T* s, const T* w, const float* rstd, T* dx, float* dweight, float* partial, cudaStream_t stream)
 {
-    const bool vec = backward_vectors(o);
     const Team t = backward_team(o);
+    const bool vec = t.full;
     cudaError_t err;
     const int splits = norm_partials(o);
     note_launch();
@@ -389,9 +408,8 @@ cudaError_t backward(const NormRows& o, const T* dy, const T* ds, const T* s, co
         err = launch_kernel(kern, dim3((unsigned)o.rows), dim3(512), 0, stream, dim3(1, 1, 1), o, dy, ds, s, w, rstd, dx);
     } else {
         auto kern = t.nu == 1 ? (vec ? rmsnorm_backward_kernel<T, 1, true> : rmsnorm_backward_kernel<T, 1, false>)
-                  : t.nu == 2 ? (vec ? rmsnorm_backward_kernel<T, 2, true> : rmsnorm_backward_kernel<T, 2, false>)
-                              : rmsnorm_backward_kernel<T, 4, true>;
-        const size_t smem = kBackwardThreads >> t.log_lanes > 1 ? (size_t)t.nu * kPiece<T> * 4 << t.log_lanes : 0;      // (at most 32 KB)
+                              : (vec ? rmsnorm_backward_kernel<T, 2, true> : rmsnorm_backward_kernel<T, 2, false>);
+        const size_t smem = kBackwardThreads >> t.log_lanes > 1 ? (size_t)t.nu * kPiece<T> * 4 << t.log_lanes : 0;      // (at most 16 KB)
         err = launch_kernel(kern, dim3((unsigned)splits), dim3(kBackwardThreads), smem, stream, dim3(1, 1, 1), o, dy, ds, s, w, rstd, dx, dweight != nullptr ? partial : nullptr, t.log_lanes);
     }
     if (err != cudaSuccess || dweight == nullptr) return err;

@@ -1,9 +1,12 @@
 // Rows of fp32 or bf16 in pieces of 16 bytes, on any boundary: what the kernels that read and write rows share.
 //
-// A piece is 16 bytes of a row, counted from the row's start (8 bf16 or 4 fp32 elements).  Rows that start on 16-byte boundaries are read and written
-// piece by piece.  A row of an odd length leaves the next one on another boundary; then a piece is put together from the two aligned
-// 16 bytes that it straddles, and written as the aligned 16 bytes that it shares with its neighbour, one lane up: element by element only at the ends of
-// a warp's stretch.  (Read and written element by element, 2 bytes at a time, rows of 4095 bf16 took three times as long as rows of 4096.)
+// A piece is 16 bytes: 8 bf16 or 4 fp32 elements.  Where rows start on 16-byte boundaries and end with a whole piece (FULL), a row is a list of
+// pieces.  Otherwise a row of an odd length leaves the next one on another boundary, and there are two ways to look at it:
+//   frame    pieces of memory on 16-byte boundaries; the first starts up to N - 1 elements before the row, and elements outside the row are masked.
+//            Nothing has to be put together, as long as every tensor of a call has the same boundaries (strides that are alike modulo N).
+//   columns  pieces of the row (what a group of an 8-bit scale needs); one is put together from the two pieces of memory that it straddles, and
+//            written as the one that it shares with its neighbour, a lane up.
+// (Element by element, 2 bytes at a time, 8000 rows of 1333 bf16 took four times as long as rows of 1336.)
 //
 // No byte past the end of a tensor is read, and none outside a row is written.
 #pragma once
@@ -56,72 +59,117 @@ __device__ __forceinline__ uint32_t element_bits(const float* p) { return __floa
 __device__ __forceinline__ uint32_t element_bits(const __nv_bfloat16* p) { return *reinterpret_cast<const unsigned short*>(p); }
 // the first `left` elements at p, one by one; zeros behind them
 template <typename T>
-__device__ __noinline__ uint4 load_slowly(const T* p, int left)
+__device__ __forceinline__ uint4 load_slowly(const T* p, int left)
 {
-    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < kPiece<T>; ++i)
-        if (i < left) w[i * sizeof(T) / 4] |= element_bits(p + i) << (i * sizeof(T) % 4 * 8);
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    unsigned long long w[2] = {0, 0};
+#pragma unroll 1
+    for (int i = 0; i < left; ++i) {
+        const int byte = i * (int)sizeof(T);
+        const unsigned long long bits = (unsigned long long)element_bits(p + i) << (8 * (byte & 7));
+        if (byte < 8) w[0] |= bits; else w[1] |= bits;
+    }
+    return make_uint4((uint32_t)w[0], (uint32_t)(w[0] >> 32), (uint32_t)w[1], (uint32_t)(w[1] >> 32));
+}
+// v with zeros in the place of elements before `from` and from `to` on
+template <typename T>
+__device__ __forceinline__ uint4 only_elements(const uint4& v, int from, int to)
+{
+    auto word = [&](uint32_t w, int j) {
+        if (sizeof(T) == 4) return j >= from && j < to ? w : 0u;
+        return (2 * j >= from && 2 * j < to ? w & 0xffffu : 0u) | (2 * j + 1 >= from && 2 * j + 1 < to ? w & 0xffff0000u : 0u);
+    };
+    return make_uint4(word(v.x, 0), word(v.y, 1), word(v.z, 2), word(v.w, 3));
 }
 
-// A piece on its way.  VEC: rows start on 16-byte boundaries.  start() only issues loads, so that those of several pieces are in flight together;
-// value() puts the piece together.  at: the piece's first element; left: elements of the row from there (may be negative); end: of the tensor.
-template <typename T, bool VEC>
+// A row to read: its first element and how far it and the tensor go
+template <typename T, bool FULL>
+struct Row {
+    const T* p;
+    int cols, off, room;          // cols: below every column, frames' too, for a row of nothing; off: bytes from the boundary below p; room: bytes from there to the end of the tensor (or 2^30)
+    // tensor: nullptr for one that is not there (a row of nothing); live = false: a row of nothing
+    __device__ __forceinline__ Row(const T* tensor, long long row, long long stride, long long rows, int columns, bool live)
+    {
+        live = live && tensor != nullptr;
+        cols = live ? columns : -(1 << 30);
+        p = tensor + (live ? row * stride : 0);
+        off = FULL ? 0 : (int)(reinterpret_cast<uintptr_t>(p) & 15);
+        room = FULL ? 0 : (int)min(1ll << 30, ((rows - 1 - row) * stride + columns) * (long long)sizeof(T) + off);
+    }
+};
+
+// A piece of a row by columns, on its way: start() only issues loads, so that those of several pieces are in flight together; value() puts it together.
+template <typename T, bool FULL>
 struct Piece {
     uint4 lo, hi;
-    __device__ __forceinline__ void start(const T* at, int left, const T* end)
+    static __device__ __forceinline__ bool straddles(const Row<T, FULL>& r, int c) { return !FULL && r.off + min(r.cols - c, kPiece<T>) * (int)sizeof(T) > 16; }
+    // (a piece whose 16 or 32 bytes go past the end of the tensor is loaded element by element, in value())
+    static __device__ __forceinline__ bool inside(const Row<T, FULL>& r, int c) { return FULL || c * (int)sizeof(T) + (straddles(r, c) ? 32 : 16) <= r.room; }
+    __device__ __forceinline__ void start(const Row<T, FULL>& r, int c)
     {
+        const uint4* from = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(r.p + c) - r.off);
+        const bool in = c < r.cols && inside(r, c);
         lo = make_uint4(0, 0, 0, 0);
-        if (VEC) {
-            if (left >= kPiece<T>) lo = *reinterpret_cast<const uint4*>(at);
-        } else {
+        if (in) lo = from[0];
+        if (!FULL) {
             hi = make_uint4(0, 0, 0, 0);
-            const int off = (int)(reinterpret_cast<uintptr_t>(at) & 15);
-            const char* from = reinterpret_cast<const char*>(at) - off;
-            const bool all = left >= kPiece<T> && from + (off ? 32 : 16) <= reinterpret_cast<const char*>(end);
-            if (all) lo = *reinterpret_cast<const uint4*>(from);
-            if (all && off) hi = *reinterpret_cast<const uint4*>(from + 16);
+            if (in && straddles(r, c)) hi = from[1];
         }
     }
-    __device__ __forceinline__ uint4 value(const T* at, int left, const T* end) const
+    __device__ __forceinline__ uint4 value(const Row<T, FULL>& r, int c) const
     {
-        uint4 v = lo;
-        if (VEC) {
-            if (left > 0 && left < kPiece<T>) v = load_slowly(at, left);
-        } else {
-            const int off = (int)(reinterpret_cast<uintptr_t>(at) & 15);
-            v = shifted16(lo, hi, off);
-            if (left > 0 && (left < kPiece<T> || reinterpret_cast<const char*>(at) - off + (off ? 32 : 16) > reinterpret_cast<const char*>(end))) v = load_slowly(at, left);
-        }
+        if (FULL) return lo;
+        uint4 v = shifted16(lo, hi, r.off);
+        const int left = r.cols - c;
+        if (left < kPiece<T>) v = only_elements<T>(v, 0, left);
+        if (left > 0 && !inside(r, c)) v = load_slowly(r.p + c, min(left, kPiece<T>));
         return v;
     }
 };
 
+// A piece of a row by its frame: N elements from column c on, where c is -off / size, N - off / size, ...
+template <typename T, bool FULL>
+struct FramePiece {
+    uint4 v;
+    __device__ __forceinline__ void start(const Row<T, FULL>& r, int c)
+    {
+        v = make_uint4(0, 0, 0, 0);
+        if (c < r.cols && (FULL || c * (int)sizeof(T) + r.off + 16 <= r.room)) v = *reinterpret_cast<const uint4*>(r.p + c);
+    }
+    __device__ __forceinline__ uint4 value(const Row<T, FULL>& r, int c) const
+    {
+        if (FULL || (c >= 0 && c + kPiece<T> <= r.cols)) return v;
+        uint4 u = v;
+        if (c < r.cols && c * (int)sizeof(T) + r.off + 16 > r.room) {        // the last piece of the tensor; c < 0: one row that is shorter than a piece
+            u = load_slowly(r.p + max(c, 0), r.cols - max(c, 0));
+            if (c < 0) u = shifted16(make_uint4(0, 0, 0, 0), u, 16 + c * (int)sizeof(T));
+        }
+        return only_elements<T>(u, -c, r.cols - c);
+    }
+};
+
+// elements [from, to) of a piece
 template <typename T>
-__device__ __noinline__ void store_slowly(T* p, uint4 v, int from, int to)
+__device__ __forceinline__ void store_slowly(T* p, const uint4& v, int from, int to)
 {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < kPiece<T>; ++i)
         if (i >= from && i < to) {
-            const uint32_t bits = w[i * sizeof(T) / 4] >> (i * sizeof(T) % 4 * 8);
-            if (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(p + i) = bits;
-            else *reinterpret_cast<unsigned short*>(p + i) = (unsigned short)bits;
+            if (sizeof(T) == 4) reinterpret_cast<uint32_t*>(p)[i] = w[i & 3];
+            else reinterpret_cast<unsigned short*>(p)[i] = (unsigned short)(w[i >> 1] >> 16 * (i & 1));
         }
 }
-// Writes the piece at `at`, of which the row has `left` elements.  All lanes of a warp call; neighbours in a stretch of 1 << log_lanes lanes (5: the
-// warp) hold neighbouring pieces of a row.
-template <typename T, bool VEC>
+// Writes a piece by columns: at, its first element, of which the row has `left` elements.  All lanes of a warp call; neighbours in a stretch of
+// 1 << log_lanes lanes (5: the warp) hold neighbouring pieces of a row.
+template <typename T, bool FULL>
 __device__ __forceinline__ void store_piece(T* at, int left, const uint4& v, int log_lanes)
 {
     constexpr int N = kPiece<T>;
-    if (VEC) {
-        if (left >= N) *reinterpret_cast<uint4*>(at) = v;
-        else if (left > 0) store_slowly(at, v, 0, left);
+    if (FULL) {
+        if (left > 0) *reinterpret_cast<uint4*>(at) = v;
         return;
     }
-    const int off = (int)(reinterpret_cast<uintptr_t>(at) & 15), lane = threadIdx.x & ((1 << min(log_lanes, 5)) - 1), last = (1 << min(log_lanes, 5)) - 1;
+    const int off = (int)(reinterpret_cast<uintptr_t>(at) & 15), last = (1 << min(log_lanes, 5)) - 1, lane = threadIdx.x & last;
     const int head = (16 - off) / (int)sizeof(T);            // elements up to the next boundary
     uint4 p;
     p.x = __shfl_up_sync(0xffffffffu, v.x, 1); p.y = __shfl_up_sync(0xffffffffu, v.y, 1);
@@ -133,6 +181,13 @@ __device__ __forceinline__ void store_piece(T* at, int left, const uint4& v, int
         const int from = whole ? head : 0, to = off != 0 && next ? head : min(left, N);
         if (from < to) store_slowly(at, v, from, to);
     }
+}
+// Writes a piece by its frame, N elements from column c on; row: the row's first element
+template <typename T, bool FULL>
+__device__ __forceinline__ void store_frame(T* row, int c, int cols, const uint4& v)
+{
+    if (FULL ? c < cols : c >= 0 && c + kPiece<T> <= cols) *reinterpret_cast<uint4*>(row + c) = v;
+    else if (!FULL && c < cols) store_slowly(row + c, v, max(0, -c), min(kPiece<T>, cols - c));
 }
 
 }  // namespace gaconv
