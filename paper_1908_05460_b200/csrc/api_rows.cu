@@ -41,9 +41,16 @@ gaconv_status_t packed_layout(const gaconv_conv_desc_t* desc, int32_t method, Ge
     gaconv_status_t st = make_geom(desc, g);
     if (st != GACONV_OK) return st;
     if (desc->x_layout != GACONV_X_NHWC || (long long)g->n * g->h > 0x7fffffffll / g->w || g->c > (1 << 30)) return GACONV_ERR_UNSUPPORTED;
+    L->fused = false;
     L->reads = method != GACONV_METHOD_ZERO && method != GACONV_METHOD_RANDOM;
     // (ALGO_DIRECT and the one-pass TF32 mode name kernels of the plain form)
-    L->fused = method == GACONV_METHOD_EXACT && desc->algo != GACONV_ALGO_DIRECT && desc->math == GACONV_MATH_DEFAULT && plan_packed(*g, desc->dy_layout == GACONV_DY_NPQK, &L->plan);
+    if (method == GACONV_METHOD_EXACT && desc->algo != GACONV_ALGO_DIRECT && desc->math == GACONV_MATH_DEFAULT) {
+        const bool npqk = desc->dy_layout == GACONV_DY_NPQK;
+        double tensor = 0, fma = 0;
+        PackedPlan other;
+        L->fused = plan_packed(*g, npqk, &L->plan, &tensor);
+        if (plan_packed_fma(*g, npqk, &other, &fma) && desc->algo != GACONV_ALGO_TENSOR && (!L->fused || fma < tensor)) { L->plan = other; L->fused = true; }
+    }
     if (L->fused) { L->inner = 0; L->total = align_up(kWsDataOffset, 256) + L->plan.partial_bytes + L->plan.dy_bytes; return GACONV_OK; }
     if ((st = method_workspace(desc, method, kNoLimit, &L->inner)) != GACONV_OK) return st;
     L->inner = align_up(L->inner, 256);
@@ -114,8 +121,10 @@ gaconv_status_t gaconv_dw_from_packed(int32_t method, const void* codes, const v
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     if (L.fused) {
         char *ws = static_cast<char*>(desc->workspace), *partial = ws + align_up(kWsDataOffset, 256);
-        return launch_packed(codes, scales, format, dy, dw, reinterpret_cast<float*>(partial), partial + L.plan.partial_bytes, reinterpret_cast<uint32_t*>(ws), g, L.plan, cs) == cudaSuccess
-                   ? GACONV_OK : GACONV_ERR_CUDA;
+        float* sums = reinterpret_cast<float*>(align_up(reinterpret_cast<size_t>(partial), 256));          // (a workspace starts on 16 bytes; the plans have room)
+        const cudaError_t err = L.plan.fma ? launch_packed_fma(codes, scales, format, dy, dw, sums, g, desc->dy_layout == GACONV_DY_NPQK, L.plan, cs)
+                                           : launch_packed(codes, scales, format, dy, dw, sums, partial + L.plan.partial_bytes, reinterpret_cast<uint32_t*>(ws), g, L.plan, cs);
+        return err == cudaSuccess ? GACONV_OK : GACONV_ERR_CUDA;
     }
     gaconv_conv_desc_t inner = *desc;
     inner.workspace_bytes = L.inner;

@@ -211,9 +211,14 @@ cudaError_t launch_act_unpack(const void* codes, const void* scales, void* x, co
 // ---- filter gradient of a linear layer from X in 8 bits, on tcgen05 ----
 struct PackedPlan {
     size_t partial_bytes, dy_bytes;         // workspace: sums of split tiles, packed copy of dY
-    alignas(8) unsigned char opaque[64];    // private to packed_dw.cu
+    bool fma;                               // on the FP32 pipes
+    alignas(8) unsigned char opaque[64];    // private to packed_dw.cu, or packed_fma.cu
 };
-bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan);       // false: not such a layer, or a gradient in another order
+// false: not such a layer.  cycles: the planners' estimates
+bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycles);
+bool plan_packed_fma(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycles);
+cudaError_t launch_packed_fma(const void* codes, const void* scales, int format, const void* dy, float* dw, float* partial, const Geom& g, bool dy_npqk, const PackedPlan& plan,
+                              cudaStream_t stream);
 cudaError_t launch_packed(const void* codes, const void* scales, int format, const void* dy, float* dw, float* partial, void* dy_scratch, uint32_t* status,
                           const Geom& g, const PackedPlan& plan, cudaStream_t stream);
 

@@ -48,7 +48,7 @@ template <int CG, int PLANES> struct Config {
     static constexpr int cols = 128 * CG, halves = PLANES == 3 ? 1 : 2, rows = halves * kRows;
     static constexpr int dy_stage = 2 * PLANES * halves * kTile, dys = 3, turneds = PLANES == 3 ? 2 : 4, raws = PLANES == 3 ? 4 : 3;
     static constexpr int raw = rows * 128 + rows * 8;               // 128 channels in 8 bits, and the two words around the four scales of each row
-    static constexpr int turned_at = dys * dy_stage, raw_at = turned_at + turneds * 2 * kTile, bytes = raw_at + raws * raw;
+    static constexpr int turned_at = dys * dy_stage, raw_at = turned_at + turneds * 2 * kTile, out_at = raw_at + raws * raw, bytes = out_at + 8 * 1024;
     static constexpr int epoch = PLANES == 3 ? 4 : 8;               // stages of dY: chains of 48 or 64 MMAs
     // registers of a thread by role; their sum over the warps is within what the block is launched with (96 each)
     static constexpr int regs_control = 48, regs_turn = CG == 2 ? 56 : 80, regs_sum = CG == 2 ? 160 : 104;
@@ -454,7 +454,29 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
             }
             if (!ok) break;
             const bool whole = unit < P.full || P.splits == 1;
-            if (k < P.k) {
+            const float a = P.alpha;
+            const bool sectors = P.ws_c == 1 && (P.ws_k & 7) == 0 && (P.c & 7) == 0 && (reinterpret_cast<uintptr_t>(P.dw) & 31) == 0;
+            if (whole && !sectors && P.ws_c == 1) {
+                // Rows of dW on any boundary: eight channels of 32 outputs turn in shared memory, and a store writes eight channels of four outputs (a lane a
+                // row, 32 sectors a store, took 12 us longer on 46 rows, 1652 -> 439)
+                const uint32_t buf = base + C::out_at + (warp - 12) * 1024;
+                float* out = P.dw + (k - lane) * P.ws_k + c0;
+#pragma unroll
+                for (int i = 0; i < H; i += 8) {
+                    store_shared16(buf + lane * 32, __float_as_uint(a * sum[i]), __float_as_uint(a * sum[i + 1]), __float_as_uint(a * sum[i + 2]), __float_as_uint(a * sum[i + 3]));
+                    store_shared16(buf + lane * 32 + 16, __float_as_uint(a * sum[i + 4]), __float_as_uint(a * sum[i + 5]), __float_as_uint(a * sum[i + 6]), __float_as_uint(a * sum[i + 7]));
+                    __syncwarp();
+                    const int c = i + (lane & 7);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int o = 4 * j + (lane >> 3);
+                        float v;
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(buf + j * 128 + lane * 4) : "memory");
+                        if (k - lane + o < P.k && c0 + c < P.c) out[o * P.ws_k + c] = v;
+                    }
+                    __syncwarp();
+                }
+            } else if (k < P.k) {
                 if (!whole) {
                     // [tail unit][output][channel]
                     float* out = P.partial + ((size_t)(unit - P.full) * (128 * CG) + rank * 128 + row) * C::cols + half * H;
@@ -465,14 +487,12 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
                                          "f"(sum[i + 3]), "f"(sum[i + 4]), "f"(sum[i + 5]), "f"(sum[i + 6]), "f"(sum[i + 7]) : "memory");
                 } else {
                     float* out = P.dw + k * P.ws_k + c0 * P.ws_c;
-                    const float a = P.alpha;
-                    const bool sectors = P.ws_c == 1 && (P.ws_k & 7) == 0 && (reinterpret_cast<uintptr_t>(P.dw) & 31) == 0;
 #pragma unroll
                     for (int i = 0; i < H; i += 8) {
-                        if (sectors && c0 + i + 8 <= P.c) {
+                        if (sectors && c0 + i < P.c) {
                             asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + i), "f"(a * sum[i]), "f"(a * sum[i + 1]), "f"(a * sum[i + 2]),
                                          "f"(a * sum[i + 3]), "f"(a * sum[i + 4]), "f"(a * sum[i + 5]), "f"(a * sum[i + 6]), "f"(a * sum[i + 7]) : "memory");
-                        } else {
+                        } else if (!sectors) {
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
                                 if (c0 + i + e < P.c) out[(i + e) * P.ws_c] = a * sum[i + e];
@@ -565,8 +585,9 @@ cudaError_t launch(const CUtensorMap& map_dy, const CUtensorMap& map_x, const Pa
 }  // namespace
 
 // Tiles of 256 x 256 by CTA pairs where they leave the GPU less idle than tiles of 128 x 128, splits where tiles are few.
-// The estimate counts cycles: stages, and what a round and a split cost beside them.
-bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan)
+// The estimate counts cycles: stages, and what a round, a split and a packing pass cost beside them (us, measured / estimated at 1.9 GHz: 512 rows 512->512
+// 8.5 / 8.1, 8192 rows 1024->4096 58.6 / 56, 4099 rows 1000->1333 27.8 / 28, 131072 rows 64->64 14.5 / 14.7).
+bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycles)
 {
     if (g.r != 1 || g.s != 1 || g.stride_h != 1 || g.stride_w != 1 || g.pad_h != 0 || g.pad_w != 0) return false;
     const long long rows = (long long)g.n * g.p * g.q;
@@ -586,13 +607,16 @@ bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan)
         const long long tiles = (long long)H.tiles_c * ceil_div(g.k, 128 * cg);
         if (tiles > 1 << 24) continue;
         const int clusters = std::max(1, sms / cg);
-        const double stage = cg == 2 ? 1250 : 1000, fixed = 4000, block = 128.0 * 128 * cg * 4 / 20;
+        const double stage = cg == 2 ? 1450 : 1100, fixed = 7500, block = 128.0 * 128 * cg * 4 / 20;
         H.full = (int)(tiles / clusters * clusters);
         const int tail = (int)(tiles - H.full);
-        for (int s = 1; s <= std::min(H.chunks, std::max(1, tail == 0 ? 1 : 4 * clusters / std::max(1, tail))); ++s) {
+        for (int r = 0; r <= 4; ++r) {          // no split, or as many as give the tail r rounds
+            const int s = r == 0 || tail == 0 ? 1 : std::min(H.chunks, r * clusters / tail);
+            if (s < 1 || (r > 0 && s == 1)) continue;
             const double rounds = std::ceil((double)tail * s / clusters);
             double cost = (double)(H.full / clusters) * H.chunks * stage + rounds * (ceil_div(H.chunks, s) * stage + 600) + fixed + block;
-            if (s > 1) cost += 3000 + (double)tail * s * 128 * 128 * cg * cg * 4 / (clusters * cg) / 20;
+            if (pack) cost += 3000 + (double)rows * g.k * (g.bf16 ? 4 : 10) / 2600;
+            if (s > 1) cost += 5500 + (double)tail * s * 128 * 128 * cg * cg * 4 / (clusters * cg) / 20;
             if (best.units != 0 && cost >= best_cost) continue;
             best_cost = cost;
             H.splits = s; H.tail = tail;
@@ -604,17 +628,18 @@ bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan)
     if (best.units == 0) return false;
     plan->partial_bytes = best.splits == 1 ? 0 : align_up((size_t)best.tail * best.splits * (128 * best.cg) * (128 * best.cg) * sizeof(float) + 256, 256);
     plan->dy_bytes = pack ? align_up((size_t)rows * round_up(g.k, 8) * (g.bf16 ? 2 : 6), 256) : 0;
+    plan->fma = false;
+    *cycles = best_cost;
     memcpy(plan->opaque, &best, sizeof(best));
     return true;
 }
 
 cudaError_t launch_packed(const void* codes, const void* scales, int format, const void* dy, float* dw, float* partial, void* dy_scratch, uint32_t* status, const Geom& g,
-                          const PackedPlan& plan, cudaStream_t stream)
+                          const PackedPlan& plan, cudaStream_t stream)          // partial lies on 32 bytes, dy_scratch on 16
 {
     PackedHost H;
     memcpy(&H, plan.opaque, sizeof(H));
     PackedParams P{};
-    partial = reinterpret_cast<float*>(align_up(reinterpret_cast<size_t>(partial), 256));          // (a workspace starts on 16 bytes)
     P.scales = static_cast<const uint8_t*>(scales);
     P.dw = dw; P.partial = partial; P.status = status;
     P.rows = (int)((long long)g.n * g.p * g.q); P.c = g.c; P.k = g.k; P.groups = act_groups(g.c);
