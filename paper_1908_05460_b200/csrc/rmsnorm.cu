@@ -17,14 +17,14 @@ namespace gaconv {
 namespace {
 
 // Sum over the threads of a team, the same bits in each.  `part`: two rows of one float a warp, taken in turn so that one barrier a sum is enough.
-__device__ __forceinline__ float team_sum(float v, int log_lanes, float (*part)[16], int& turn)
+__device__ __forceinline__ float team_sum(float v, int lanes, int team, float (*part)[16], int& turn)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (log_lanes > 5) {
-        const int warp = threadIdx.x >> 5, team = threadIdx.x >> log_lanes, n = 1 << (log_lanes - 5), first = team << (log_lanes - 5);
-        if ((threadIdx.x & 31) == 0) part[turn][warp] = v;
-        asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(1 << log_lanes) : "memory");
+    if (lanes > 32) {
+        const int n = lanes >> 5, first = team * n;
+        if ((threadIdx.x & 31) == 0) part[turn][threadIdx.x >> 5] = v;
+        asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(lanes) : "memory");
         v = 0.f;
         for (int i = 0; i < n; ++i) v += part[turn][first + i];
         turn ^= 1;
@@ -63,89 +63,96 @@ __device__ __forceinline__ uint4 load_weight(const T* __restrict__ w, int c, int
     return shifted16(make_uint4(0, 0, 0, 0), load_slowly(w, min(cols, kPiece<T> + c)), 16 + c * (int)sizeof(T));
 }
 
+// Blocks stay and their teams take rows in turn, the next one's loads on their way while a row is worked on.  Where rows are not whole pieces a team's
+// rows are a multiple of N apart: they have one frame, and the weight's pieces in it stay in registers.
 template <typename T, int NU, bool FULL>
 __global__ void __launch_bounds__(512)
-rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __restrict__ w, T* sum, T* y, uint8_t* codes, uint8_t* scales, float* rstd, int log_lanes)
+rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __restrict__ w, T* sum, T* y, uint8_t* codes, uint8_t* scales, float* rstd, int lanes)
 {
     constexpr int N = kPiece<T>;
     __shared__ float part[2][16];
-    __shared__ uint4 s_head[FULL ? 1 : NU + 1][16];
+    __shared__ uint4 s_head[FULL ? 1 : 2][FULL ? 1 : NU][16];
     pdl_release_next_grid();
-    const int lanes = 1 << log_lanes, l = threadIdx.x & (lanes - 1), warp = threadIdx.x >> 5;
-    const long long row = (long long)blockIdx.x * (blockDim.x >> log_lanes) + (threadIdx.x >> log_lanes);
-    const bool live = row < o.rows;          // (teams without a row go along: shuffles and barriers are shared)
-    const long long r = live ? row : 0;
-    const int cols = live ? o.cols : 0;
-    const Row<T, FULL> rx(x, r, o.x_stride, o.rows, o.cols, live), rr(res, r, o.r_stride, o.rows, o.cols, live);
-    const int shift = FULL ? 0 : rx.off / (int)sizeof(T);          // the frame: columns -shift, N - shift, ...
-    int turn = 0;
+    const int team = threadIdx.x / lanes, l = threadIdx.x - team * lanes, teams = blockDim.x / lanes, warp = threadIdx.x >> 5;
+    const long long step = (long long)gridDim.x * teams;
+    long long row = (long long)blockIdx.x * teams + team;
+    const int shift = FULL ? 0 : (int)(row * o.x_stride % N);          // the frame: columns -shift, N - shift, ...
+    int turn = 0, parity = 0;
     pdl_wait_prior_grid();
-    uint4 v[NU];
-    {
-        FramePiece<T, FULL> px[NU], pr[NU];
+    uint4 vw[NU];
 #pragma unroll
-        for (int i = 0; i < NU; ++i) px[i].start(rx, N * (i * lanes + l) - shift);
-        if (res != nullptr) {
+    for (int i = 0; i < NU; ++i) vw[i] = load_weight<T, FULL>(w, N * (i * lanes + l) - shift, o.cols);
+    uint4 vn[FULL ? 1 : NU];          // a warp's last lane: the weight of the piece behind its own
 #pragma unroll
-            for (int i = 0; i < NU; ++i) pr[i].start(rr, N * (i * lanes + l) - shift);
+    for (int i = 0; i < (FULL ? 0 : NU); ++i) vn[i] = load_weight<T, FULL>(w, N * (i * lanes + l) - shift + N, (l & 31) == 31 ? o.cols : 0);
+    FramePiece<T, FULL> px[NU], pr[NU];
+    auto start = [&](long long row) {
+        const Row<T, FULL> rx(x, row, o.x_stride, o.rows, o.cols, row < o.rows), rr(res, row, o.r_stride, o.rows, o.cols, row < o.rows);
+#pragma unroll
+        for (int i = 0; i < NU; ++i) { px[i].start(rx, N * (i * lanes + l) - shift); pr[i].start(rr, N * (i * lanes + l) - shift); }
+    };
+    start(row);
+    for (; row < o.rows; row += step) {
+        uint4 v[NU];
+        {
+            const Row<T, FULL> rx(x, row, o.x_stride, o.rows, o.cols, true), rr(res, row, o.r_stride, o.rows, o.cols, true);
+#pragma unroll
+            for (int i = 0; i < NU; ++i) {
+                const int c = N * (i * lanes + l) - shift;
+                v[i] = px[i].value(rx, c);
+                if (res != nullptr) v[i] = add_pieces<T>(v[i], pr[i].value(rr, c));
+            }
         }
+        start(row + step);
+        if (sum != nullptr) {
+#pragma unroll
+            for (int i = 0; i < NU; ++i) store_frame<T, FULL>(sum + row * o.s_stride, N * (i * lanes + l) - shift, o.cols, v[i]);
+        }
+        float q = 0.f;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int c = N * (i * lanes + l) - shift;
-            v[i] = px[i].value(rx, c);
-            if (res != nullptr) v[i] = add_pieces<T>(v[i], pr[i].value(rr, c));
+            float f[N], t = 0.f;
+            to_floats<T>(v[i], f);
+#pragma unroll
+            for (int j = 0; j < N; ++j) t = fmaf(f[j], f[j], t);
+            q += t;
+            if (!FULL && (l & 31) == 0) s_head[parity][i][warp] = v[i];
         }
-    }
-    if (sum != nullptr) {
+        if (!FULL) __syncwarp();
+        q = team_sum(q, lanes, team, part, turn);          // (and a barrier of the team, where it has several warps)
+        const float rs = 1.f / sqrtf(q / (float)o.cols + o.eps);
+        if (l == 0 && rstd != nullptr) rstd[row] = rs;
+        auto output = [&](const uint4& s, const uint4& weight) {
+            float f[N], t[N];
+            to_floats<T>(weight, t);
+            to_floats<T>(s, f);
 #pragma unroll
-        for (int i = 0; i < NU; ++i) store_frame<T, FULL>(sum + r * o.s_stride, N * (i * lanes + l) - shift, cols, v[i]);
-    }
-    float q = 0.f;
+            for (int j = 0; j < N; ++j) t[j] = f[j] * rs * t[j];
+            return from_floats<T>(t);
+        };
 #pragma unroll
-    for (int i = 0; i < NU; ++i) {
-        float f[N], t = 0.f;
-        to_floats<T>(v[i], f);
-#pragma unroll
-        for (int j = 0; j < N; ++j) t = fmaf(f[j], f[j], t);
-        q += t;
-        if (!FULL && (l & 31) == 0) s_head[i][warp] = v[i];
-    }
-    if (!FULL) {
-        if (l == 0) s_head[NU][warp] = make_uint4(0, 0, 0, 0);
-        __syncwarp();
-    }
-    q = team_sum(q, log_lanes, part, turn);          // (and a barrier of the team, where it has several warps)
-    const float rs = 1.f / sqrtf(q / (float)o.cols + o.eps);
-    if (live && l == 0 && rstd != nullptr) rstd[r] = rs;
-    const int pitch = live ? o.pitch : 0;
-    auto output = [&](const uint4& s, int c) {
-        float f[N], t[N];
-        to_floats<T>(load_weight<T, FULL>(w, c, o.cols), t);
-        to_floats<T>(s, f);
-#pragma unroll
-        for (int j = 0; j < N; ++j) t[j] = f[j] * rs * t[j];
-        return from_floats<T>(t);
-    };
-#pragma unroll
-    for (int i = 0; i < NU; ++i) {
-        const int c = N * (i * lanes + l);
-        uint4 out = output(v[i], c - shift);
-        if (y != nullptr) store_frame<T, FULL>(y + r * o.y_stride, c - shift, cols, out);
-        if (codes != nullptr) {
-            if (!FULL) {        // from the frame to columns: with what the next piece of the frame has, a lane up or, for a warp's last lane, of its neighbour's first
-                uint4 next;
-                next.x = __shfl_down_sync(0xffffffffu, out.x, 1); next.y = __shfl_down_sync(0xffffffffu, out.y, 1);
-                next.z = __shfl_down_sync(0xffffffffu, out.z, 1); next.w = __shfl_down_sync(0xffffffffu, out.w, 1);
-                if ((l & 31) == 31) {
-                    const bool wraps = l == lanes - 1;
-                    next = output(s_head[wraps ? i + 1 : i][wraps ? warp - (lanes >> 5) + 1 : warp + 1], c - shift + N);
+        for (int i = 0; i < NU; ++i) {
+            const int c = N * (i * lanes + l);
+            uint4 out = output(v[i], vw[i]);
+            if (y != nullptr) store_frame<T, FULL>(y + row * o.y_stride, c - shift, o.cols, out);
+            if (codes != nullptr) {
+                if (!FULL) {        // from the frame to columns: with what the next piece of the frame has, a lane up or, for a warp's last lane, of its neighbour's first
+                    uint4 next;
+                    next.x = __shfl_down_sync(0xffffffffu, out.x, 1); next.y = __shfl_down_sync(0xffffffffu, out.y, 1);
+                    next.z = __shfl_down_sync(0xffffffffu, out.z, 1); next.w = __shfl_down_sync(0xffffffffu, out.w, 1);
+                    if ((l & 31) == 31) {
+                        const bool wraps = l == lanes - 1;
+                        next = make_uint4(0, 0, 0, 0);
+                        if (!wraps || i + 1 < NU) next = output(s_head[parity][wraps && i + 1 < NU ? i + 1 : i][wraps ? warp - (lanes >> 5) + 1 : warp + 1], vn[FULL ? 0 : i]);
+                    }
+                    out = shifted16(out, next, shift * (int)sizeof(T));
                 }
-                out = shifted16(out, next, shift * (int)sizeof(T));
+                float t[N];
+                to_floats<T>(out, t);
+                store_codes<N>(o, t, codes, scales, row, c, o.pitch - c);
             }
-            float t[N];
-            to_floats<T>(out, t);
-            store_codes<N>(o, t, codes, scales, r, c, pitch - c);
         }
+        parity ^= 1;
     }
 }
 
@@ -178,7 +185,7 @@ rmsnorm_forward_long_kernel(const NormRows o, const T* x, const T* res, const T*
         for (int j = 0; j < N; ++j) t = fmaf(f[j], f[j], t);
         q += t;
     }
-    q = team_sum(q, 9, part, turn);          // (a barrier: the neighbours' stores of a shared 16 bytes are seen below)
+    q = team_sum(q, 512, 0, part, turn);          // (a barrier: the neighbours' stores of a shared 16 bytes are seen below)
     const float rs = 1.f / sqrtf(q / (float)o.cols + o.eps);
     if (threadIdx.x == 0 && rstd != nullptr) rstd[r] = rs;
     const Row<T, FULL> again(sum != nullptr ? sum : x, r, sum != nullptr ? o.s_stride : o.x_stride, o.rows, o.cols, true);
@@ -206,13 +213,13 @@ rmsnorm_forward_long_kernel(const NormRows o, const T* x, const T* res, const T*
 // formed again after the mean.
 template <typename T, int NU, bool FULL>
 __global__ void __launch_bounds__(512)
-rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, const T* __restrict__ w, const float* __restrict__ rstd, T* dx, float* __restrict__ partial, int log_lanes)
+rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, const T* __restrict__ w, const float* __restrict__ rstd, T* dx, float* __restrict__ partial, int lanes)
 {
     constexpr int N = kPiece<T>;
     extern __shared__ float s_dw[];
     __shared__ float part[2][16];
     pdl_release_next_grid();
-    const int lanes = 1 << log_lanes, l = threadIdx.x & (lanes - 1), team = threadIdx.x >> log_lanes, teams = blockDim.x >> log_lanes;
+    const int team = threadIdx.x / lanes, l = threadIdx.x - team * lanes, teams = blockDim.x / lanes;
     float acc[NU][N];
 #pragma unroll
     for (int i = 0; i < NU; ++i)
@@ -265,7 +272,7 @@ rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, 
             }
             dot += sum;
         }
-        dot = team_sum(dot, log_lanes, part, turn) * inv;
+        dot = team_sum(dot, lanes, team, part, turn) * inv;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
             float g[N], h[N], t[N], d[N];
@@ -329,7 +336,7 @@ rmsnorm_backward_long_kernel(const NormRows o, const T* dy, const T* ds, const T
                 store_piece<T, FULL>(dx + row * o.x_stride + c, o.cols - c, from_floats<T>(d), 9);
             }
         }
-        if (pass == 0) dot = team_sum(dot, 9, part, turn) / (float)o.cols;
+        if (pass == 0) dot = team_sum(dot, 512, 0, part, turn) / (float)o.cols;
     }
 }
 // sums over a range of rows, a thread a channel: grid (channels / 256, ranges)
@@ -349,52 +356,54 @@ rmsnorm_weight_long_kernel(const NormRows o, const T* dy, const T* s, const floa
 }
 
 // ---------------------------------------------------------------- host side
-struct Team { int log_lanes, nu; bool full; };          // nu = 0: a row by blocks, twice
-// threads of a row: `most` pieces each, or fewer where that leaves SMs without work.  strides: of the tensors in the call.
+struct Team { int lanes, nu; bool full; };          // nu = 0: a row by blocks, twice
+constexpr int kMaxTeam = 512;
+// Threads of a row, a multiple of 32: two pieces each, one where that leaves SMs without work, four (forward) for rows that do not fit otherwise.
+// strides: of the tensors in the call.
 Team team_of(const NormRows& o, int most, long long a, long long b, long long c, long long d)
 {
     const int n = o.bf16 ? 8 : 4;
-    Team t{5, 0, o.cols % n == 0 && a % n == 0 && b % n == 0 && c % n == 0 && d % n == 0};
+    Team t{0, 0, o.cols % n == 0 && a % n == 0 && b % n == 0 && c % n == 0 && d % n == 0};
     const int pieces = t.full ? o.cols / n : (o.cols + 2 * n - 2) / n;         // (a frame starts up to n - 1 elements early)
-    while (t.log_lanes < 9 && most << t.log_lanes < pieces) ++t.log_lanes;
-    while (t.log_lanes < 9 && 1 << t.log_lanes < pieces && o.rows << t.log_lanes < 148 * 512) ++t.log_lanes;
-    const int per = (pieces + (1 << t.log_lanes) - 1) >> t.log_lanes;
-    if (t.full || (a % n == b % n && a % n == c % n && a % n == d % n)) t.nu = per <= 1 ? 1 : per <= 2 ? 2 : per <= 4 && most == 4 ? 4 : 0;
+    auto lanes = [&](int nu) { return (pieces + 32 * nu - 1) / (32 * nu) * 32; };
+    if (!t.full && (a % n != b % n || a % n != c % n || a % n != d % n)) return t;
+    t.nu = lanes(1) == 32 || (lanes(1) <= kMaxTeam && o.rows * lanes(2) < 148 * 512) ? 1 : lanes(2) <= kMaxTeam ? 2 : lanes(4) <= kMaxTeam && most == 4 ? 4 : 0;
+    if (t.nu != 0) t.lanes = lanes(t.nu);
     return t;
 }
-constexpr int kBackwardThreads = 512;
-Team backward_team(const NormRows& o) { return team_of(o, 2, o.y_stride, o.s_stride, o.x_stride, o.s_stride); }
-int backward_blocks(const NormRows& o, const Team& t)
+// Blocks for teams that stay: as many as fit the SMs, and such that a team's rows have one frame
+int team_blocks(const NormRows& o, const Team& t, long long stride, int teams, int most)
 {
-    const int teams = kBackwardThreads >> t.log_lanes, n = o.bf16 ? 8 : 4;
+    const int n = o.bf16 ? 8 : 4;
     const long long need = (o.rows + teams - 1) / teams;
-    int most = device_sms();
-    while (!t.full && most > 1 && (long long)most * teams * o.s_stride % n != 0) --most;         // (a team's rows have one frame)
-    return (int)std::min<long long>(need, most);
+    if (need <= most) return (int)need;
+    while (!t.full && most > 1 && (long long)most * teams * stride % n != 0) --most;
+    return most;
 }
+Team backward_team(const NormRows& o) { return team_of(o, 2, o.y_stride, o.s_stride, o.x_stride, o.s_stride); }
+int backward_blocks(const NormRows& o, const Team& t) { return team_blocks(o, t, o.s_stride, kMaxTeam / t.lanes, device_sms()); }
 
 template <typename T>
 cudaError_t forward(const NormRows& o, const T* x, const T* res, const T* w, T* sum, T* y, uint8_t* codes, uint8_t* scales, float* rstd, cudaStream_t stream)
 {
     const Team t = team_of(o, 4, o.x_stride, res ? o.r_stride : o.x_stride, sum ? o.s_stride : o.x_stride, y ? o.y_stride : o.x_stride);
-    const bool vec = t.full;
     note_launch();
     if (t.nu == 0) {
-        auto kern = vec ? rmsnorm_forward_long_kernel<T, true> : rmsnorm_forward_long_kernel<T, false>;
+        auto kern = t.full ? rmsnorm_forward_long_kernel<T, true> : rmsnorm_forward_long_kernel<T, false>;
         return launch_kernel(kern, dim3((unsigned)o.rows), dim3(512), 0, stream, dim3(1, 1, 1), o, x, res, w, sum, y, codes, scales, rstd);
     }
-    const int threads = std::max(128, 1 << t.log_lanes), teams = threads >> t.log_lanes;
-    auto kern = t.nu == 1 ? (vec ? rmsnorm_forward_kernel<T, 1, true> : rmsnorm_forward_kernel<T, 1, false>)
-              : t.nu == 2 ? (vec ? rmsnorm_forward_kernel<T, 2, true> : rmsnorm_forward_kernel<T, 2, false>)
-                          : (vec ? rmsnorm_forward_kernel<T, 4, true> : rmsnorm_forward_kernel<T, 4, false>);
-    return launch_kernel(kern, dim3((unsigned)((o.rows + teams - 1) / teams)), dim3(threads), 0, stream, dim3(1, 1, 1), o, x, res, w, sum, y, codes, scales, rstd, t.log_lanes);
+    const int teams = std::max(1, 128 / t.lanes), threads = teams * t.lanes;
+    auto kern = t.nu == 1 ? (t.full ? rmsnorm_forward_kernel<T, 1, true> : rmsnorm_forward_kernel<T, 1, false>)
+              : t.nu == 2 ? (t.full ? rmsnorm_forward_kernel<T, 2, true> : rmsnorm_forward_kernel<T, 2, false>)
+                          : (t.full ? rmsnorm_forward_kernel<T, 4, true> : rmsnorm_forward_kernel<T, 4, false>);
+    const int per_sm = std::max(1, kMaxTeam / threads);
+    return launch_kernel(kern, dim3((unsigned)team_blocks(o, t, o.x_stride, teams, per_sm * device_sms())), dim3(threads), 0, stream, dim3(1, 1, 1), o, x, res, w, sum, y, codes, scales, rstd, t.lanes);
 }
 
 template <typename T>
 cudaError_t backward(const NormRows& o, const T* dy, const T* ds, const T* s, const T* w, const float* rstd, T* dx, float* dweight, float* partial, cudaStream_t stream)
 {
     const Team t = backward_team(o);
-    const bool vec = t.full;
     cudaError_t err;
     const int splits = norm_partials(o);
     note_launch();
@@ -404,13 +413,14 @@ cudaError_t backward(const NormRows& o, const T* dy, const T* ds, const T* s, co
             if (err != cudaSuccess) return err;
             note_launch();
         }
-        auto kern = vec ? rmsnorm_backward_long_kernel<T, true> : rmsnorm_backward_long_kernel<T, false>;
+        auto kern = t.full ? rmsnorm_backward_long_kernel<T, true> : rmsnorm_backward_long_kernel<T, false>;
         err = launch_kernel(kern, dim3((unsigned)o.rows), dim3(512), 0, stream, dim3(1, 1, 1), o, dy, ds, s, w, rstd, dx);
     } else {
-        auto kern = t.nu == 1 ? (vec ? rmsnorm_backward_kernel<T, 1, true> : rmsnorm_backward_kernel<T, 1, false>)
-                              : (vec ? rmsnorm_backward_kernel<T, 2, true> : rmsnorm_backward_kernel<T, 2, false>);
-        const size_t smem = kBackwardThreads >> t.log_lanes > 1 ? (size_t)t.nu * kPiece<T> * 4 << t.log_lanes : 0;      // (at most 16 KB)
-        err = launch_kernel(kern, dim3((unsigned)splits), dim3(kBackwardThreads), smem, stream, dim3(1, 1, 1), o, dy, ds, s, w, rstd, dx, dweight != nullptr ? partial : nullptr, t.log_lanes);
+        auto kern = t.nu == 1 ? (t.full ? rmsnorm_backward_kernel<T, 1, true> : rmsnorm_backward_kernel<T, 1, false>)
+                              : (t.full ? rmsnorm_backward_kernel<T, 2, true> : rmsnorm_backward_kernel<T, 2, false>);
+        const int teams = kMaxTeam / t.lanes;
+        const size_t smem = teams > 1 ? (size_t)t.nu * kPiece<T> * 4 * t.lanes : 0;      // (at most 16 KB)
+        err = launch_kernel(kern, dim3((unsigned)splits), dim3((unsigned)(teams * t.lanes)), smem, stream, dim3(1, 1, 1), o, dy, ds, s, w, rstd, dx, dweight != nullptr ? partial : nullptr, t.lanes);
     }
     if (err != cudaSuccess || dweight == nullptr) return err;
     return reduce_splits(partial, dweight, (size_t)o.cols, splits, 1.f, stream);

@@ -57,18 +57,15 @@ template <> __device__ __forceinline__ uint4 from_floats<__nv_bfloat16>(const fl
 
 __device__ __forceinline__ uint32_t element_bits(const float* p) { return __float_as_uint(*p); }
 __device__ __forceinline__ uint32_t element_bits(const __nv_bfloat16* p) { return *reinterpret_cast<const unsigned short*>(p); }
-// the first `left` elements at p, one by one; zeros behind them
+// the first `left` elements at p, one by one (all loads in flight together); zeros behind them
 template <typename T>
 __device__ __forceinline__ uint4 load_slowly(const T* p, int left)
 {
-    unsigned long long w[2] = {0, 0};
-#pragma unroll 1
-    for (int i = 0; i < left; ++i) {
-        const int byte = i * (int)sizeof(T);
-        const unsigned long long bits = (unsigned long long)element_bits(p + i) << (8 * (byte & 7));
-        if (byte < 8) w[0] |= bits; else w[1] |= bits;
-    }
-    return make_uint4((uint32_t)w[0], (uint32_t)(w[0] >> 32), (uint32_t)w[1], (uint32_t)(w[1] >> 32));
+    uint32_t e[kPiece<T>];
+#pragma unroll
+    for (int i = 0; i < kPiece<T>; ++i) e[i] = i < left ? element_bits(p + i) : 0u;
+    if constexpr (sizeof(T) == 4) return make_uint4(e[0], e[1], e[2], e[3]);
+    else return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
 }
 // v with zeros in the place of elements before `from` and from `to` on
 template <typename T>
