@@ -127,20 +127,26 @@ def _check(status: int, where: str):
 
 
 def _ptr(t):
-    if t is None:
-        return None
-    if isinstance(t, int):
+    try:
+        return t.data_ptr()
+    except AttributeError:          # None, or an address
         return t
-    return t.data_ptr()
 
 
 # the handle alone: torch.cuda.current_stream() builds a Stream object around it, 3 us a call where this takes 0.2
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", None)        # torch.cuda.current_device() without its look at whether CUDA runs, 0.25 us
+_cuda_runs = False
 
 
 def _stream(stream):
+    global _cuda_runs
     if stream is None:
-        return _raw_stream(torch.cuda.current_device()) if _raw_stream else torch.cuda.current_stream().cuda_stream
+        if _cuda_runs:
+            return _raw_stream(_device())
+        device = torch.cuda.current_device()          # (the first call starts CUDA, or says why it cannot)
+        _cuda_runs = _raw_stream is not None and _device is not None
+        return _raw_stream(device) if _raw_stream else torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -242,11 +248,11 @@ def gaconv_act_sizes(desc: RowsDesc) -> tuple[int, int]:
 
 
 def gaconv_act_pack(x, codes, scales, desc: RowsDesc, stream=None):
-    _check(load().gaconv_act_pack(_ptr(x), _ptr(codes), _ptr(scales), ctypes.byref(desc), _stream(stream)), "gaconv_act_pack")
+    _check((_lib or load()).gaconv_act_pack(_ptr(x), _ptr(codes), _ptr(scales), ctypes.byref(desc), _stream(stream)), "gaconv_act_pack")
 
 
 def gaconv_act_unpack(codes, scales, x, desc: RowsDesc, stream=None):
-    _check(load().gaconv_act_unpack(_ptr(codes), _ptr(scales), _ptr(x), ctypes.byref(desc), _stream(stream)), "gaconv_act_unpack")
+    _check((_lib or load()).gaconv_act_unpack(_ptr(codes), _ptr(scales), _ptr(x), ctypes.byref(desc), _stream(stream)), "gaconv_act_unpack")
 
 
 def gaconv_packed_workspace_size(desc: ConvDesc, method: int) -> int:
@@ -265,12 +271,12 @@ def attach_packed_workspace(desc: ConvDesc, methods=(METHOD_EXACT,), device="cud
 
 
 def gaconv_dw_from_packed(method: int, codes, scales, fmt: int, dy, dw, desc: ConvDesc, seed: int = 0, stream=None):
-    _check(load().gaconv_dw_from_packed(method, _ptr(codes), _ptr(scales), fmt, _ptr(dy), _ptr(dw), ctypes.byref(desc), seed,
+    _check((_lib or load()).gaconv_dw_from_packed(method, _ptr(codes), _ptr(scales), fmt, _ptr(dy), _ptr(dw), ctypes.byref(desc), seed,
                                         _stream(stream)), "gaconv_dw_from_packed")
 
 
 def gaconv_rmsnorm_forward(x, residual, weight, sum_, y, codes, scales, rstd, desc: RowsDesc, stream=None):
-    _check(load().gaconv_rmsnorm_forward(_ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_), _ptr(y), _ptr(codes), _ptr(scales),
+    _check((_lib or load()).gaconv_rmsnorm_forward(_ptr(x), _ptr(residual), _ptr(weight), _ptr(sum_), _ptr(y), _ptr(codes), _ptr(scales),
                                          _ptr(rstd), ctypes.byref(desc), _stream(stream)), "gaconv_rmsnorm_forward")
 
 
@@ -286,7 +292,7 @@ def rmsnorm_workspace(desc: RowsDesc, device="cuda") -> torch.Tensor:
 
 
 def gaconv_rmsnorm_backward(dy, dsum, sum_, weight, rstd, dx, dweight, desc: RowsDesc, workspace=None, stream=None):
-    _check(load().gaconv_rmsnorm_backward(_ptr(dy), _ptr(dsum), _ptr(sum_), _ptr(weight), _ptr(rstd), _ptr(dx), _ptr(dweight),
+    _check((_lib or load()).gaconv_rmsnorm_backward(_ptr(dy), _ptr(dsum), _ptr(sum_), _ptr(weight), _ptr(rstd), _ptr(dx), _ptr(dweight),
                                           ctypes.byref(desc), _ptr(workspace), 0 if workspace is None else workspace.numel(),
                                           _stream(stream)), "gaconv_rmsnorm_backward")
 
