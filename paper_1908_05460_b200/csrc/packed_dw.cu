@@ -598,7 +598,7 @@ bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycles)
     const bool last = dy_npqk || g.k == 1 || g.p * g.q == 1;
     const bool pack = !g.bf16 || g.k % 8 != 0 || !last;
     if (pack && rows * round_up(g.k, 8) > 0x7fffffffll) return false;
-    for (int cg = 1; cg <= (g.bf16 ? 2 : 1); ++cg) {
+    for (int cg = 1; cg <= 2; ++cg) {
         PackedHost H{};
         H.cg = cg; H.f32 = !g.bf16; H.pack = pack; H.npqk = last;
         const int stage_rows = g.bf16 ? Config<1, 1>::rows : Config<1, 3>::rows;
@@ -607,7 +607,7 @@ bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycles)
         const long long tiles = (long long)H.tiles_c * ceil_div(g.k, 128 * cg);
         if (tiles > 1 << 24) continue;
         const int clusters = std::max(1, sms / cg);
-        const double stage = cg == 2 ? 1450 : 1100, fixed = 7500, block = 128.0 * 128 * cg * 4 / 20;
+        const double stage = H.f32 ? (cg == 2 ? 2000 : 1600) : cg == 2 ? 1450 : 1100, fixed = 7500, block = 128.0 * 128 * cg * 4 / 20;
         H.full = (int)(tiles / clusters * clusters);
         const int tail = (int)(tiles - H.full);
         for (int r = 0; r <= 4; ++r) {          // no split, or as many as give the tail r rounds
@@ -662,7 +662,7 @@ cudaError_t launch_packed(const void* codes, const void* scales, int format, con
     if (!encode(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, g.k, (size_t)kp * 2, planes, 64, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !encode(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, act_pitch(g.c), act_pitch(g.c), 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE))
         return cudaErrorInvalidValue;
-    err = H.f32 ? launch<1, 3>(map_dy, map_x, P, format, H.grid, stream) : H.cg == 2 ? launch<2, 1>(map_dy, map_x, P, format, H.grid, stream)
+    err = H.f32 ? (H.cg == 2 ? launch<2, 3>(map_dy, map_x, P, format, H.grid, stream) : launch<1, 3>(map_dy, map_x, P, format, H.grid, stream)) : H.cg == 2 ? launch<2, 1>(map_dy, map_x, P, format, H.grid, stream)
                 : launch<1, 1>(map_dy, map_x, P, format, H.grid, stream);
     if (err != cudaSuccess) return err;
     note_launch();

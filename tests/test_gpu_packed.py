@@ -188,6 +188,18 @@ def test_linear(m, c, k, dtype, fmt):
     Case(linear(m, c, k), dtype, fmt).check()
 
 
+# more tiles than CTA pairs (whole tiles and split ones), splits of few and of many rows, a tile and a bit
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m, c, k", [(1500, 2050, 2600), (700, 2304, 2048), (2500, 1000, 1333), (300, 257, 2000), (9000, 256, 257), (129, 1100, 1030), (40000, 64, 72), (3000, 520, 128)])
+def test_linear_of_many_tiles(m, c, k, dtype):
+    Case(linear(m, c, k), dtype, B.ACT_INT8 if m % 2 else B.ACT_E4M3).check()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_linear_transposed_result_of_many_tiles(dtype):
+    Case(linear(700, 1300, 1100), dtype, B.ACT_E4M3, dw_layout=B.DW_RSCK, alpha=0.5).check()
+
+
 @pytest.mark.parametrize("dw_layout", [B.DW_KRSC, B.DW_KCRS, B.DW_RSCK])
 @pytest.mark.parametrize("dy_layout", [B.DY_NKPQ, B.DY_NPQK])
 @pytest.mark.parametrize("dtype", DTYPES)
