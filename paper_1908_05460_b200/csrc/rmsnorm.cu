@@ -209,7 +209,7 @@ rmsnorm_forward_long_kernel(const NormRows o, const T* x, const T* res, const T*
 
 // Backward.  A block stays and its teams take rows in turn; a thread keeps the sums over rows of dy h for its channels, which the
 // teams of a block add up in order at the end: partial[block][cols].  A team's rows are a multiple of N apart, so that they have one frame, and a thread the
-// same channels in each.  The three tensors of a row are loaded while the row before is worked on, and kept as they are: the products of the first half are
+// same channels in each.  (One block writes dweight itself.)  The three tensors of a row are loaded while the row before is worked on, and kept as they are: the products of the first half are
 // formed again after the mean.
 template <typename T, int NU, bool FULL>
 __global__ void __launch_bounds__(512)
@@ -283,21 +283,21 @@ rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, 
         }
     }
     if (partial == nullptr) return;
+    // the teams' sums, in order; team t's at s_dw + t * cols
+    float* mine = s_dw + (size_t)team * o.cols;
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+        const int c = N * (i * lanes + l) - shift;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (c + j >= 0 && c + j < o.cols) mine[c + j] = acc[i][j];
+    }
+    __syncthreads();
     float* out = partial + (size_t)blockIdx.x * o.cols;
-    for (int t = 0; t < teams; ++t) {
-        if (team == t) {
-#pragma unroll
-            for (int i = 0; i < NU; ++i) {
-                const int c = N * (i * lanes + l) - shift;
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    if (c + j < 0 || c + j >= o.cols) continue;
-                    const float v = t == 0 ? acc[i][j] : s_dw[c + j] + acc[i][j];
-                    (t + 1 < teams ? s_dw : out)[c + j] = v;
-                }
-            }
-        }
-        __syncthreads();
+    for (int c = threadIdx.x; c < o.cols; c += blockDim.x) {
+        float v = s_dw[c];
+        for (int t = 1; t < teams; ++t) v += s_dw[t * o.cols + c];
+        out[c] = v;
     }
 }
 
@@ -419,10 +419,11 @@ cudaError_t backward(const NormRows& o, const T* dy, const T* ds, const T* s, co
         auto kern = t.nu == 1 ? (t.full ? rmsnorm_backward_kernel<T, 1, true> : rmsnorm_backward_kernel<T, 1, false>)
                               : (t.full ? rmsnorm_backward_kernel<T, 2, true> : rmsnorm_backward_kernel<T, 2, false>);
         const int teams = kMaxTeam / t.lanes;
-        const size_t smem = teams > 1 ? (size_t)t.nu * kPiece<T> * 4 * t.lanes : 0;      // (at most 16 KB)
+        const size_t smem = sizeof(float) * (size_t)teams * o.cols;          // (at most 512 threads' sums: 32 KB)
+        if (splits == 1) partial = dweight;
         err = launch_kernel(kern, dim3((unsigned)splits), dim3((unsigned)(teams * t.lanes)), smem, stream, dim3(1, 1, 1), o, dy, ds, s, w, rstd, dx, dweight != nullptr ? partial : nullptr, t.lanes);
     }
-    if (err != cudaSuccess || dweight == nullptr) return err;
+    if (err != cudaSuccess || dweight == nullptr || (t.nu != 0 && splits == 1)) return err;
     return reduce_splits(partial, dweight, (size_t)o.cols, splits, 1.f, stream);
 }
 
