@@ -166,10 +166,10 @@ bool plan_packed_fma(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycl
             const int splits = (int)std::min<long long>(std::min<long long>(chunks, room), 256);
             const long long per = (chunks + splits - 1) / splits;
             const int used = (int)((chunks + per - 1) / per);
-            const double rounds = std::ceil((double)blocks * used / (4.0 * sms)), busy = std::min(4.0, std::ceil((double)blocks * used / sms));
+            const double rounds = std::max(1.0, (double)blocks * used / (4.0 * sms)), busy = std::min(4.0, std::ceil((double)blocks * used / sms));
             // a chunk of a block alone on an SM, and what each of up to three others sharing it adds
-            const double part = std::min(1.0, (double)rows / chunk), alone = 1600 + 1800 * part, shared = (400 + 1400 * part) * (chunk == 32 ? 1.5 : 1.0);
-            double cost = 2600 + per * rounds * (alone + shared * (busy - 1));
+            const double part = std::min(1.0, (double)rows / chunk), alone = 1600 + 1800 * part, shared = (400 + 1400 * part) * (chunk == 32 ? 2.0 : 1.0);
+            double cost = 2600 + per * rounds * (alone + shared * (busy - 1)) + 4.0 * g.k * g.c / (sms * (g.c % 4 != 0 ? 8 : 20));
             if (used > 1) cost += 4000 + 4.0 * used * g.k * g.c / (sms * 20);
             if (best.tk != 0 && cost >= best_cost) continue;
             best_cost = cost;

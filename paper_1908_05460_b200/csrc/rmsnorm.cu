@@ -20,7 +20,10 @@ namespace {
 __device__ __forceinline__ float team_sum(float v, int lanes, int team, float (*part)[16], int& turn)
 {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = 16; o > 0; o >>= 1) {
+        const float other = __shfl_xor_sync(0xffffffffu, v, o);
+        if (o < lanes) v += other;
+    }
     if (lanes > 32) {
         const int n = lanes >> 5, first = team * n;
         if ((threadIdx.x & 31) == 0) part[turn][threadIdx.x >> 5] = v;
@@ -75,8 +78,9 @@ rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __re
     pdl_release_next_grid();
     const int team = threadIdx.x / lanes, l = threadIdx.x - team * lanes, teams = blockDim.x / lanes, warp = threadIdx.x >> 5;
     const long long step = (long long)gridDim.x * teams;
-    long long row = (long long)blockIdx.x * teams + team;
-    const int shift = FULL ? 0 : (int)(row * o.x_stride % N);          // the frame: columns -shift, N - shift, ...
+    long long first = (long long)blockIdx.x * teams;          // row of the block's first team; its teams go along in step, with or without a row
+    const int shift = FULL ? 0 : (int)((first + team) * o.x_stride % N);          // the frame: columns -shift, N - shift, ...
+    const bool edge = lanes >= 32 ? (l & 31) == 31 : l == lanes - 1;                // the next piece of the frame is not a lane up
     int turn = 0, parity = 0;
     pdl_wait_prior_grid();
     uint4 vw[NU];
@@ -84,18 +88,21 @@ rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __re
     for (int i = 0; i < NU; ++i) vw[i] = load_weight<T, FULL>(w, N * (i * lanes + l) - shift, o.cols);
     uint4 vn[FULL ? 1 : NU];          // a warp's last lane: the weight of the piece behind its own
 #pragma unroll
-    for (int i = 0; i < (FULL ? 0 : NU); ++i) vn[i] = load_weight<T, FULL>(w, N * (i * lanes + l) - shift + N, (l & 31) == 31 ? o.cols : 0);
+    for (int i = 0; i < (FULL ? 0 : NU); ++i) vn[i] = load_weight<T, FULL>(w, N * (i * lanes + l) - shift + N, edge ? o.cols : 0);
     FramePiece<T, FULL> px[NU], pr[NU];
     auto start = [&](long long row) {
         const Row<T, FULL> rx(x, row, o.x_stride, o.rows, o.cols, row < o.rows), rr(res, row, o.r_stride, o.rows, o.cols, row < o.rows);
 #pragma unroll
         for (int i = 0; i < NU; ++i) { px[i].start(rx, N * (i * lanes + l) - shift); pr[i].start(rr, N * (i * lanes + l) - shift); }
     };
-    start(row);
-    for (; row < o.rows; row += step) {
+    start(first + team);
+    for (; first < o.rows; first += step) {
+        const long long row = first + team;
+        const bool live = row < o.rows;
+        const int cols = live ? o.cols : 0, pitch = live ? o.pitch : 0;
         uint4 v[NU];
         {
-            const Row<T, FULL> rx(x, row, o.x_stride, o.rows, o.cols, true), rr(res, row, o.r_stride, o.rows, o.cols, true);
+            const Row<T, FULL> rx(x, row, o.x_stride, o.rows, o.cols, live), rr(res, row, o.r_stride, o.rows, o.cols, live);
 #pragma unroll
             for (int i = 0; i < NU; ++i) {
                 const int c = N * (i * lanes + l) - shift;
@@ -106,7 +113,7 @@ rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __re
         start(row + step);
         if (sum != nullptr) {
 #pragma unroll
-            for (int i = 0; i < NU; ++i) store_frame<T, FULL>(sum + row * o.s_stride, N * (i * lanes + l) - shift, o.cols, v[i]);
+            for (int i = 0; i < NU; ++i) store_frame<T, FULL>(sum + row * o.s_stride, N * (i * lanes + l) - shift, cols, v[i]);
         }
         float q = 0.f;
 #pragma unroll
@@ -121,7 +128,7 @@ rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __re
         if (!FULL) __syncwarp();
         q = team_sum(q, lanes, team, part, turn);          // (and a barrier of the team, where it has several warps)
         const float rs = 1.f / sqrtf(q / (float)o.cols + o.eps);
-        if (l == 0 && rstd != nullptr) rstd[row] = rs;
+        if (live && l == 0 && rstd != nullptr) rstd[row] = rs;
         auto output = [&](const uint4& s, const uint4& weight) {
             float f[N], t[N];
             to_floats<T>(weight, t);
@@ -134,13 +141,13 @@ rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __re
         for (int i = 0; i < NU; ++i) {
             const int c = N * (i * lanes + l);
             uint4 out = output(v[i], vw[i]);
-            if (y != nullptr) store_frame<T, FULL>(y + row * o.y_stride, c - shift, o.cols, out);
+            if (y != nullptr) store_frame<T, FULL>(y + row * o.y_stride, c - shift, cols, out);
             if (codes != nullptr) {
                 if (!FULL) {        // from the frame to columns: with what the next piece of the frame has, a lane up or, for a warp's last lane, of its neighbour's first
                     uint4 next;
                     next.x = __shfl_down_sync(0xffffffffu, out.x, 1); next.y = __shfl_down_sync(0xffffffffu, out.y, 1);
                     next.z = __shfl_down_sync(0xffffffffu, out.z, 1); next.w = __shfl_down_sync(0xffffffffu, out.w, 1);
-                    if ((l & 31) == 31) {
+                    if (edge) {
                         const bool wraps = l == lanes - 1;
                         next = make_uint4(0, 0, 0, 0);
                         if (!wraps || i + 1 < NU) next = output(s_head[parity][wraps && i + 1 < NU ? i + 1 : i][wraps ? warp - (lanes >> 5) + 1 : warp + 1], vn[FULL ? 0 : i]);
@@ -149,7 +156,7 @@ rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __re
                 }
                 float t[N];
                 to_floats<T>(out, t);
-                store_codes<N>(o, t, codes, scales, row, c, o.pitch - c);
+                store_codes<N>(o, t, codes, scales, live ? row : 0, c, pitch - c);
             }
         }
         parity ^= 1;
@@ -227,8 +234,8 @@ rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, 
         for (int j = 0; j < N; ++j) acc[i][j] = 0.f;
     int turn = 0;
     const long long step = (long long)gridDim.x * teams;
-    long long row = (long long)blockIdx.x * teams + team;
-    const int shift = FULL ? 0 : (int)((row * o.s_stride) % N);
+    long long first = (long long)blockIdx.x * teams;          // row of the block's first team; its teams go along in step, with or without a row
+    const int shift = FULL ? 0 : (int)((first + team) * o.s_stride % N);
     pdl_wait_prior_grid();
     uint4 vw[NU];
 #pragma unroll
@@ -246,12 +253,14 @@ rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, 
         }
         if (live) rs_next = __ldg(rstd + row);
     };
-    start(row);
-    for (; row < o.rows; row += step) {
+    start(first + team);
+    for (; first < o.rows; first += step) {
+        const long long row = first + team;
+        const bool live = row < o.rows;
         uint4 vg[NU], vs[NU], vd[NU];
         const float rs = rs_next;
         {
-            const Row<T, FULL> rg(dy, row, o.y_stride, o.rows, o.cols, true), rh(s, row, o.s_stride, o.rows, o.cols, true), rd(ds, row, o.s_stride, o.rows, o.cols, true);
+            const Row<T, FULL> rg(dy, row, o.y_stride, o.rows, o.cols, live), rh(s, row, o.s_stride, o.rows, o.cols, live), rd(ds, row, o.s_stride, o.rows, o.cols, live);
 #pragma unroll
             for (int i = 0; i < NU; ++i) {
                 const int c = N * (i * lanes + l) - shift;
@@ -279,7 +288,7 @@ rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, 
             to_floats<T>(vg[i], g); to_floats<T>(vs[i], h); to_floats<T>(vw[i], t); to_floats<T>(vd[i], d);
 #pragma unroll
             for (int j = 0; j < N; ++j) d[j] = fmaf(rs, g[j] * t[j] - h[j] * rs * dot, d[j]);
-            store_frame<T, FULL>(dx + row * o.x_stride, N * (i * lanes + l) - shift, o.cols, from_floats<T>(d));
+            store_frame<T, FULL>(dx + row * o.x_stride, N * (i * lanes + l) - shift, live ? o.cols : 0, from_floats<T>(d));
         }
     }
     if (partial == nullptr) return;
@@ -358,7 +367,7 @@ rmsnorm_weight_long_kernel(const NormRows o, const T* dy, const T* s, const floa
 // ---------------------------------------------------------------- host side
 struct Team { int lanes, nu; bool full; };          // nu = 0: a row by blocks, twice
 constexpr int kMaxTeam = 512;
-// Threads of a row, a multiple of 32: two pieces each, one where that leaves SMs without work, four (forward) for rows that do not fit otherwise.
+// Threads of a row, a multiple of 32 or, for short rows, 8 or 16: two pieces each, one where that leaves SMs without work, four (forward) for rows that do not fit otherwise.
 // strides: of the tensors in the call.
 Team team_of(const NormRows& o, int most, long long a, long long b, long long c, long long d)
 {
@@ -368,7 +377,7 @@ Team team_of(const NormRows& o, int most, long long a, long long b, long long c,
     auto lanes = [&](int nu) { return (pieces + 32 * nu - 1) / (32 * nu) * 32; };
     if (!t.full && (a % n != b % n || a % n != c % n || a % n != d % n)) return t;
     t.nu = lanes(1) == 32 || (lanes(1) <= kMaxTeam && o.rows * lanes(2) < 148 * 512) ? 1 : lanes(2) <= kMaxTeam ? 2 : lanes(4) <= kMaxTeam && most == 4 ? 4 : 0;
-    if (t.nu != 0) t.lanes = lanes(t.nu);
+    if (t.nu != 0) t.lanes = pieces <= 8 ? 8 : pieces <= 16 ? 16 : lanes(t.nu);
     return t;
 }
 // Blocks for teams that stay: as many as fit the SMs, and such that a team's rows have one frame
