@@ -367,7 +367,7 @@ rmsnorm_weight_long_kernel(const NormRows o, const T* dy, const T* s, const floa
 // ---------------------------------------------------------------- host side
 struct Team { int lanes, nu; bool full; };          // nu = 0: a row by blocks, twice
 constexpr int kMaxTeam = 512;
-// Threads of a row, a multiple of 32 or, for short rows, 8 or 16: two pieces each, one where that leaves SMs without work, four (forward) for rows that do not fit otherwise.
+// Threads of a row, a multiple of 32 or, for short rows, 8 or 16: two pieces each, one where that leaves SMs without work, four (forward) for long rows.
 // strides: of the tensors in the call.
 Team team_of(const NormRows& o, int most, long long a, long long b, long long c, long long d)
 {
@@ -376,7 +376,7 @@ Team team_of(const NormRows& o, int most, long long a, long long b, long long c,
     const int pieces = t.full ? o.cols / n : (o.cols + 2 * n - 2) / n;         // (a frame starts up to n - 1 elements early)
     auto lanes = [&](int nu) { return (pieces + 32 * nu - 1) / (32 * nu) * 32; };
     if (!t.full && (a % n != b % n || a % n != c % n || a % n != d % n)) return t;
-    t.nu = lanes(1) == 32 || (lanes(1) <= kMaxTeam && o.rows * lanes(2) < 148 * 512) ? 1 : lanes(2) <= kMaxTeam ? 2 : lanes(4) <= kMaxTeam && most == 4 ? 4 : 0;
+    t.nu = lanes(1) == 32 || (lanes(1) <= kMaxTeam && o.rows * lanes(2) < 148 * 512) ? 1 : lanes(2) <= (most == 4 ? kMaxTeam / 2 : kMaxTeam) ? 2 : lanes(4) <= kMaxTeam && most == 4 ? 4 : 0;
     if (t.nu != 0) t.lanes = pieces <= 8 ? 8 : pieces <= 16 ? 16 : lanes(t.nu);
     return t;
 }
@@ -405,7 +405,14 @@ cudaError_t forward(const NormRows& o, const T* x, const T* res, const T* w, T* 
     auto kern = t.nu == 1 ? (t.full ? rmsnorm_forward_kernel<T, 1, true> : rmsnorm_forward_kernel<T, 1, false>)
               : t.nu == 2 ? (t.full ? rmsnorm_forward_kernel<T, 2, true> : rmsnorm_forward_kernel<T, 2, false>)
                           : (t.full ? rmsnorm_forward_kernel<T, 4, true> : rmsnorm_forward_kernel<T, 4, false>);
-    const int per_sm = std::max(1, kMaxTeam / threads);
+    // blocks that an SM holds, asked once per kernel, size and device (all devices of a process alike)
+    static std::atomic<int> resident[2][3][kMaxTeam / 32 + 1];
+    std::atomic<int>& known = resident[t.full][t.nu / 2][threads / 32];
+    int per_sm = known.load(std::memory_order_relaxed);
+    if (per_sm == 0) {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, threads, 0) != cudaSuccess || per_sm < 1) per_sm = 1;
+        known.store(per_sm, std::memory_order_relaxed);
+    }
     return launch_kernel(kern, dim3((unsigned)team_blocks(o, t, o.x_stride, teams, per_sm * device_sms())), dim3(threads), 0, stream, dim3(1, 1, 1), o, x, res, w, sum, y, codes, scales, rstd, t.lanes);
 }
 
