@@ -215,7 +215,7 @@ typedef enum { GACONV_ACT_E4M3 = 0, GACONV_ACT_INT8 = 1 } gaconv_act_format_t;
 
 typedef struct gaconv_rows_desc {
     uint32_t struct_size;              /* = sizeof(gaconv_rows_desc_t); versions the struct               */
-    int32_t  cols;                     /* channels of a row, at least 1                                   */
+    int32_t  cols;                     /* channels of a row, 1 to 2^28                                      */
     int64_t  rows;                     /* 0 to 2^31 - 1; 0: the call writes nothing (a weight gradient: zeros) */
     int32_t  dtype;                    /* gaconv_dtype_t of the plain tensors                             */
     int32_t  format;                   /* gaconv_act_format_t of codes                                    */

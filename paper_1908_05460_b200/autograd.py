@@ -30,18 +30,19 @@ class _Conv2dFilterGrad(torch.autograd.Function):
         ctx.module = module
         ctx.packed, ctx.shape = None, x.shape
         if module.checkpoint is None:
-            ctx.save_for_backward(x, weight)
+            ctx.save_for_backward(weight, x)
+        elif ctx.needs_input_grad[1]:
+            kept, ctx.packed = PackedActivation.pack(x.permute(0, 2, 3, 1), module.checkpoint).saved()
+            ctx.save_for_backward(weight, *kept)
         else:
-            if ctx.needs_input_grad[1]:
-                ctx.packed = PackedActivation.pack(x.permute(0, 2, 3, 1), module.checkpoint)
             ctx.save_for_backward(weight)
         return F.conv2d(x, weight, None, module.stride, module.padding)
 
     @staticmethod
     def backward(ctx, dy):
-        *x, weight = ctx.saved_tensors
+        weight, *kept = ctx.saved_tensors
         m = ctx.module
-        x = x[0] if x else None
+        x = kept[0] if len(kept) == 1 else None              # (one tensor: the input; two: its codes and scales; none: not needed)
         dx = None
         if ctx.needs_input_grad[0]:
             if x is None:        # (the gradient of the input does not read it; its shape and memory order count)
@@ -54,7 +55,7 @@ class _Conv2dFilterGrad(torch.autograd.Function):
                                                      (True, False, False))[0]
         dw = None
         if ctx.needs_input_grad[1]:
-            dw = m.filter_gradient(x, dy) if ctx.packed is None else m.packed_filter_gradient(ctx.packed, ctx.shape, dy)
+            dw = m.filter_gradient(x, dy) if ctx.packed is None else m.packed_filter_gradient(PackedActivation.restored(kept, ctx.packed), ctx.shape, dy)
         return dx, dw, None
 
 
@@ -135,21 +136,21 @@ class _LinearFilterGrad(torch.autograd.Function):
     def forward(ctx, x, weight, bias, packed, fmt):
         if ctx.needs_input_grad[1] and packed is None and x.numel() > 0:
             packed = PackedActivation.pack(x, fmt)
-        ctx.packed = packed if ctx.needs_input_grad[1] else None
-        ctx.save_for_backward(weight)
+        kept, ctx.packed = packed.saved() if ctx.needs_input_grad[1] and packed is not None else ((), None)
+        ctx.save_for_backward(weight, *kept)
         return F.linear(x, weight, bias)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        weight, = ctx.saved_tensors
+        weight, *kept = ctx.saved_tensors
         dx = dw = db = None
         if ctx.needs_input_grad[0]:
             dx = dy.matmul(weight)
         if ctx.needs_input_grad[2]:
             db = dy.reshape(-1, dy.shape[-1]).sum(0)
         if ctx.needs_input_grad[1]:
-            dw = torch.zeros_like(weight) if dy.numel() == 0 else linear_filter_gradient(ctx.packed, dy).to(weight.dtype)
+            dw = torch.zeros_like(weight) if dy.numel() == 0 else linear_filter_gradient(PackedActivation.restored(kept, ctx.packed), dy).to(weight.dtype)
         return dx, dw, db, None, None
 
 

@@ -22,7 +22,7 @@ gaconv_status_t check_rows(const gaconv_rows_desc_t* d, gaconv_rows_desc_t* out)
         if (*s < d->cols) return GACONV_ERR_BAD_DESC;
         if (*s > (1ll << 40)) return GACONV_ERR_UNSUPPORTED;       // (offsets stay far below 2^63 elements)
     }
-    return d->rows > 0x7fffffffll || d->cols > (1 << 30) ? GACONV_ERR_UNSUPPORTED : GACONV_OK;
+    return d->rows > 0x7fffffffll || d->cols > (1 << 28) ? GACONV_ERR_UNSUPPORTED : GACONV_OK;
 }
 
 template <typename... P>
@@ -40,7 +40,7 @@ gaconv_status_t packed_layout(const gaconv_conv_desc_t* desc, int32_t method, Ge
 {
     gaconv_status_t st = make_geom(desc, g);
     if (st != GACONV_OK) return st;
-    if (desc->x_layout != GACONV_X_NHWC || (long long)g->n * g->h > 0x7fffffffll / g->w || g->c > (1 << 30)) return GACONV_ERR_UNSUPPORTED;
+    if (desc->x_layout != GACONV_X_NHWC || (long long)g->n * g->h > 0x7fffffffll / g->w || g->c > (1 << 28)) return GACONV_ERR_UNSUPPORTED;
     L->fused = false;
     L->reads = method != GACONV_METHOD_ZERO && method != GACONV_METHOD_RANDOM;
     // (ALGO_DIRECT and the one-pass TF32 mode name kernels of the plain form)

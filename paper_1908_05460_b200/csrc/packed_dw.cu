@@ -10,12 +10,17 @@
 // multiple of 8) are packed into the workspace first.
 //
 // A CTA pair (CG = 2) shares a tile of 256 x 256: each CTA holds 128 outputs of dY and 128 channels of X, and the pair's MMAs read both halves of X,
-// so that a turned element serves 256 outputs.  (Shared memory is the bound: for 64 rows a CTA's MMAs read 32 KB, the copies write 16 + 8, and
-// turning reads 8 and writes 16, 80 KB at 128 bytes a cycle beside the 512 cycles of the MMAs; with tiles of 128 x 128 it is as much beside 256.)
-// CG = 1: tiles of 128 x 128 for problems that would not fill the GPU with larger ones.
+// so that a turned element serves 256 outputs.  CG = 1: tiles of 128 x 128 for problems that would not fill the GPU with larger ones (16384 rows,
+// 4096 -> 4096: 515 us by pairs; 8192 rows, 1024 -> 4096: 59 by pairs, 104 by single CTAs; 512 rows, 512 -> 512: 10.5 and 8.5).
+//
+// What bounds it: 64 rows take the MMAs of a pair 512 cycles, and ~785 pass (16384 rows, 4096 -> 4096, 1065 TFLOP/s where cuBLAS on bf16 operands has 1420;
+// tensor pipe 70 % active, shared-memory banks 38 % busy, DRAM 14 %).  Turning 64 x 128 elements takes four warps ~1200 cycles, most of it latency (loads, eight
+// chains of five instructions, stores, the fence), two groups of four warps alternate, and every other time the MMAs wait for them.  What helped: rings
+// apart for dY, X and X turned; copies of 128 rows, since a warp needs 500 cycles to fill a stage however large it is; looking at a barrier before its
+// turn, since that takes 200; no cluster-wide acquire (550 -> 507 us); decoding in five instructions a pair.  A third group of warps has no registers left.
 //
 // Whoever turns X loads nothing from memory: the fence between its stores and the tensor core waits for every load that the thread has in flight
-// (loads two stages ahead in its registers: 1435 us for 16384 rows, 4096 -> 4096, where the wait alone was three times the MMAs).
+// (loads two stages ahead in its registers: 1435 us).
 //
 // The tensor core adds by truncation, so accumulators are handed over every `epoch` stages to eight warps that add them up in fp32 registers; two
 // accumulator sets alternate.  CTAs stay and take units (a tile, a range of rows) in turn; pipeline and sets run on from unit to unit, so

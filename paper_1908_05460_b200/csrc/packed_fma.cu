@@ -151,7 +151,7 @@ bool plan_packed_fma(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycl
 {
     if (g.r != 1 || g.s != 1 || g.stride_h != 1 || g.stride_w != 1 || g.pad_h != 0 || g.pad_w != 0) return false;
     const long long rows = (long long)g.n * g.p * g.q;
-    if (rows > 0x7fffff00ll) return false;
+    if (rows > 0x7ff00000ll) return false;          // (a split's last row, rounded up, stays an int)
     const int sms = g.sm_budget > 0 ? std::min(g.sm_budget, device_sms()) : device_sms();
     FmaHost best{};
     double best_cost = 0;

@@ -48,6 +48,16 @@ class PackedActivation:
     def desc(self, x_stride: int = 0) -> B.RowsDesc:
         return B.make_rows_desc(self.rows, self.cols, self.dtype, fmt=FORMATS[self.fmt], x_stride=x_stride)
 
+    def saved(self):
+        """What autograd keeps of it, and what is needed to put it together again."""
+        return (self.codes, self.scales), (self.rows, self.cols, self.dtype, self.fmt)
+
+    @classmethod
+    def restored(cls, tensors, what) -> "PackedActivation":
+        p = cls.__new__(cls)
+        (p.codes, p.scales), (p.rows, p.cols, p.dtype, p.fmt) = tensors, what
+        return p
+
     @classmethod
     def pack(cls, x: torch.Tensor, fmt: str = "e4m3") -> "PackedActivation":
         """x [..., cols], bf16 or fp32."""

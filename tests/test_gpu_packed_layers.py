@@ -257,5 +257,9 @@ def test_memory_that_is_kept():
     held = torch.cuda.memory_allocated() - before - y.numel() * 2
     assert 4096 * 1024 <= held <= 4096 * 1024 * 1.1
     del x
-    y.sum().backward()
+    loss = y.sum()
+    del y
+    loss.backward()
     assert torch.isfinite(layer.weight.grad).all()
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() - before < 4096 * 1024          # freed with the backward pass, though the loss lives on

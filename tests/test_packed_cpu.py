@@ -30,7 +30,7 @@ def test_sizes():
     ("struct_size", 8, B.ERR_BAD_DESC), ("cols", 0, B.ERR_BAD_DESC), ("cols", -3, B.ERR_BAD_DESC), ("rows", -1, B.ERR_BAD_DESC),
     ("dtype", 2, B.ERR_BAD_DESC), ("dtype", -1, B.ERR_BAD_DESC), ("format", 2, B.ERR_BAD_DESC), ("eps", -1.0, B.ERR_BAD_DESC),
     ("eps", float("nan"), B.ERR_BAD_DESC), ("x_stride", 63, B.ERR_BAD_DESC), ("r_stride", -64, B.ERR_BAD_DESC), ("s_stride", 1, B.ERR_BAD_DESC),
-    ("y_stride", 63, B.ERR_BAD_DESC), ("rows", 1 << 31, B.ERR_UNSUPPORTED), ("x_stride", 1 << 50, B.ERR_UNSUPPORTED)])
+    ("y_stride", 63, B.ERR_BAD_DESC), ("rows", 1 << 31, B.ERR_UNSUPPORTED), ("cols", (1 << 28) + 1, B.ERR_UNSUPPORTED), ("x_stride", 1 << 50, B.ERR_UNSUPPORTED)])
 def test_bad_rows_descriptors(field, value, status):
     lib, d = B.load(), B.make_rows_desc(4, 64, torch.bfloat16)
     setattr(d, field, value)
@@ -41,6 +41,12 @@ def test_bad_rows_descriptors(field, value, status):
     assert lib.gaconv_rmsnorm_forward(P, P, P, P, P, P, P, P, r, None) == status
     assert lib.gaconv_rmsnorm_backward(P, P, P, P, P, P, P, r, P, 1 << 30, None) == status
     assert lib.gaconv_rmsnorm_workspace_size(r, ctypes.byref(n)) == status
+
+
+def test_bad_types():
+    for dtype in (torch.float16, torch.int8, torch.float64):
+        with pytest.raises(TypeError):
+            B.make_rows_desc(4, 64, dtype)
 
 
 def test_bad_pointers():
