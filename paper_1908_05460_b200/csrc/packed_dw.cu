@@ -10,8 +10,9 @@
 // multiple of 8) are packed into the workspace first.
 //
 // A CTA pair (CG = 2) shares a tile of 256 x 256: each CTA holds 128 outputs of dY and 128 channels of X, and the pair's MMAs read both halves of X,
-// so that a turned element serves 256 outputs.  CG = 1: tiles of 128 x 128 for problems that would not fill the GPU with larger ones (16384 rows,
-// 4096 -> 4096: 515 us by pairs; 8192 rows, 1024 -> 4096: 59 by pairs, 104 by single CTAs; 512 rows, 512 -> 512: 10.5 and 8.5).
+// so that a turned element serves 256 outputs.  CG = 1: tiles of 128 x 128, or 128 x 64, for problems that would not fill the GPU with larger ones (us by
+// pairs, by 128 x 128, by 128 x 64: 8192 rows 1024 -> 4096 59, 104, -; 16384 rows 100 -> 1000 18.1, 15.7, 18.0; 1000 rows 1000 -> 1000 13.3, 11.7,
+// 9.8; 512 rows 512 -> 512 10.5, 8.5, 6.9: an SM writes 21 bytes a cycle, so that small results want many SMs).
 //
 // What bounds it: 64 rows take the MMAs of a pair 512 cycles, and ~785 pass (16384 rows, 4096 -> 4096, 1065 TFLOP/s where cuBLAS on bf16 operands has 1420;
 // tensor pipe 70 % active, shared-memory banks 38 % busy, DRAM 14 %).  Turning 64 x 128 elements takes four warps ~1200 cycles, most of it latency (loads, eight
@@ -49,18 +50,19 @@ constexpr int kMaxRing = 4;
 
 // Three rings: dY and X in 8 bits as they are copied, `halves` x 64 rows at a time (a warp takes ~500 cycles for its round of wait, byte count and copy, however
 // large the copy is, and the MMAs 512 for 64 rows), and X turned, 64 rows at a time.
-template <int CG, int PLANES> struct Config {
-    static constexpr int cols = 128 * CG, halves = PLANES == 3 ? 1 : 2, rows = halves * kRows;
-    static constexpr int dy_stage = 2 * PLANES * halves * kTile, dys = 3, turneds = PLANES == 3 ? 2 : 4, raws = PLANES == 3 ? 4 : 3;
-    static constexpr int raw = rows * 128 + rows * 8;               // 128 channels in 8 bits, and the two words around the four scales of each row
-    static constexpr int turned_at = dys * dy_stage, raw_at = turned_at + turneds * 2 * kTile, out_at = raw_at + raws * raw, bytes = out_at + 8 * 1024;
+template <int PLANES> constexpr int kStageRows = PLANES == 3 ? kRows : 2 * kRows;
+template <int CG, int PLANES, int XC> struct Config {           // XC: channels of X that a CTA turns
+    static constexpr int cols = XC * CG, halves = PLANES == 3 ? 1 : 2, rows = kStageRows<PLANES>, atoms = XC / 64;
+    static constexpr int dy_stage = 2 * PLANES * halves * kTile, dys = 3, turned = atoms * kTile, turneds = PLANES == 3 ? 2 : 4, raws = PLANES == 3 ? 4 : 3;
+    static constexpr int raw = rows * XC + rows * 8;                // the channels in 8 bits, and the two words around the scales of each row
+    static constexpr int turned_at = dys * dy_stage, raw_at = turned_at + turneds * turned, out_at = raw_at + raws * raw, bytes = out_at + 8 * 1024;
     static constexpr int epoch = PLANES == 3 ? 4 : 8;               // stages of dY: chains of 48 or 64 MMAs
     // registers of a thread by role; their sum over the warps is within what the block is launched with (96 each)
     static constexpr int regs_control = 48, regs_turn = CG == 2 ? 56 : 80, regs_sum = CG == 2 ? 160 : 104;
     static_assert(4 * regs_control + 8 * regs_turn + 8 * regs_sum <= 20 * 96, "registers");
     // A wait for a phase is only right once the phase before is over, which a group knows of its own stages alone: no slot passes from one group to the other
     static_assert(turneds % 2 == 0 && raws * halves % 2 == 0, "two groups turn X");
-    static_assert(dys <= kMaxRing && turneds <= kMaxRing && raws <= kMaxRing && bytes <= 225 * 1024, "shared memory");
+    static_assert(dys <= kMaxRing && turneds <= kMaxRing && raws <= kMaxRing && bytes <= 225 * 1024 && raw % 128 == 0, "shared memory");
 };
 
 struct PackedParams {
@@ -164,11 +166,11 @@ struct Walk {
     }
 };
 
-template <int CG, int PLANES, int FMT>
+template <int CG, int PLANES, int XC, int FMT>
 __global__ void __launch_bounds__(kThreads, 1)
 packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ PackedParams P)
 {
-    typedef Config<CG, PLANES> C;
+    typedef Config<CG, PLANES, XC> C;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_dy[kMaxRing], bar_free_dy[kMaxRing], bar_full[kMaxRing], bar_empty[kMaxRing], bar_raw[kMaxRing], bar_taken[kMaxRing], bar_acc[2], bar_free[2], bar_last;
     __shared__ uint32_t s_tmem;
@@ -222,8 +224,8 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
                 if (!ok) break;
                 if (elect_one()) {
                     const uint32_t bar = smem_u32(&bar_raw[st]);
-                    mbar_expect_tx(bar, C::rows * 128);
-                    tma_load_3d(base + C::raw_at + st * C::raw, &map_x, bar, (w.c0 * CG + rank) * 128, w.chunk * C::rows, 0);
+                    mbar_expect_tx(bar, C::rows * XC);
+                    tma_load_3d(base + C::raw_at + st * C::raw, &map_x, bar, (w.c0 * CG + rank) * XC, w.chunk * C::rows, 0);
                 }
                 __syncwarp();
                 if (++st == C::raws) { st = 0; ph ^= 1; }
@@ -266,8 +268,8 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
                 if (!taken) ok = mbar_wait(smem_u32(&bar_taken[st]), ph ^ 1);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                const uint32_t bar = smem_u32(&bar_raw[st]), dst = base + C::raw_at + st * C::raw + C::rows * 128;
-                const int g = (w.c0 * CG + rank) * 4;
+                const uint32_t bar = smem_u32(&bar_raw[st]), dst = base + C::raw_at + st * C::raw + C::rows * XC;
+                const int g = (w.c0 * CG + rank) * (XC / 32);
 #pragma unroll
                 for (int i = 0; i < C::rows / 32; ++i) {
                     // a row's scales lie on any byte: the one or two aligned words that hold them, no byte past the end
@@ -325,7 +327,7 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
                         ready = mbar_look(smem_u32(&bar_full[next]), ph);
                         if (h == C::halves - 1) ready_dy = mbar_look(smem_u32(&bar_dy[next_ds]), dph);
                         if (elect_one()) {
-                            const uint32_t a0 = base + ds * C::dy_stage + h * kTile, b0 = base + C::turned_at + st * 2 * kTile;
+                            const uint32_t a0 = base + ds * C::dy_stage + h * kTile, b0 = base + C::turned_at + st * C::turned;
                             const uint64_t a = hi | (lbo_dy | (a0 >> 4)), b = hi | (lbo_x | (b0 >> 4));
                             const uint32_t d = tmem + set * C::cols;
 #pragma unroll
@@ -364,12 +366,14 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
         // lower 64 channels of a row and the upper 64 of its neighbour: then neither their reads nor their writes, whose chunks are permuted by
         // the row, meet in a bank.
         regs_down<C::regs_turn>();
-        const int t = threadIdx.x & 127, mine = (warp - 4) >> 2, q = t & 7, row = (t >> 3) ^ (q >> 2);
+        // (64 channels: four pieces a row, eight lanes take a row and the next.)
+        constexpr int pieces = XC / 16, each = kRows * pieces / 128, apart = 128 / pieces;          // of a row; of a thread, so many rows apart
+        const int t = threadIdx.x & 127, mine = (warp - 4) >> 2, q = t & (pieces - 1), row = XC == 128 ? (t >> 3) ^ (q >> 2) : t >> 2;
         constexpr int advance = 2 / C::halves;          // stages from this group's rows to its next
         const uint32_t raw = base + C::raw_at, half = C::halves == 2 ? mine * kRows : 0;
-        const uint32_t from = raw + (half + row) * 128 + 16 * q;
-        // (a row's first scale lies at byte (row * groups) % 4 of its two words, the same for rows 4 apart)
-        const uint32_t scale = raw + C::rows * 128 + (half + row) * 8 + (row * P.groups & 3) + (q >> 1);
+        const uint32_t from = raw + (half + row) * XC + 16 * q;
+        // (a row's first scale lies at byte (row * groups + its group) % 4 of its two words, the same for rows 4 apart)
+        const uint32_t scale = raw + C::rows * XC + (half + row) * 8 + (q >> 1);
         const uint32_t to = base + C::turned_at + (q >> 2) * kTile + row * 128, x0 = ((2 * (q & 3)) ^ (row & 7)) << 4;
         Walk w;
         w.start(P, group);
@@ -378,26 +382,30 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
         bool ok = true, filled = false, empty = true;
         while (w.live()) {
             if (!filled) ok = mbar_wait(smem_u32(&bar_raw[rs]), rph);
-            uint4 v[4];
-            uint32_t s[4];
+            uint4 v[each];
+            uint32_t s[each];
+            const uint32_t sa = scale + rs * C::raw + ((row * P.groups + (w.c0 * CG + rank) * (XC / 32)) & 3);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[i] = load_shared16(from + rs * C::raw + i * 2048);
-                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(s[i]) : "r"(scale + rs * C::raw + i * 128) : "memory");
+            for (int i = 0; i < each; ++i) {
+                v[i] = load_shared16(from + rs * C::raw + i * apart * XC);
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(s[i]) : "r"(sa + i * apart * 8) : "memory");
             }
             if (!empty) ok = ok && pair_wait(smem_u32(&bar_empty[st]), ph ^ 1);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            const uint32_t dst = to + st * 2 * kTile;
+            const uint32_t dst = to + st * C::turned;
             const int old_st = st, old_rs = rs;
             for (st += 2; st >= C::turneds; st -= C::turneds) ph ^= 1;
             for (rs += advance; rs >= C::raws; rs -= C::raws) rph ^= 1;
             n += 2;
             filled = mbar_look(smem_u32(&bar_raw[rs]), rph);
             empty = n < C::turneds || mbar_look(smem_u32(&bar_empty[st]), ph ^ 1);
-            const bool rest = __any_sync(0xffffffffu, act_has_rest<FMT>(max(max(s[0], s[1]), max(s[2], s[3]))));
+            uint32_t top = s[0];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 1; i < each; ++i) top = max(top, s[i]);
+            const bool rest = __any_sync(0xffffffffu, act_has_rest<FMT>(top));
+#pragma unroll
+            for (int i = 0; i < each; ++i) {
                 const uint32_t s2 = act_scale2<FMT>(s[i]);
                 uint2 d[4] = {act_decode4<FMT>(v[i].x, s2), act_decode4<FMT>(v[i].y, s2), act_decode4<FMT>(v[i].z, s2), act_decode4<FMT>(v[i].w, s2)};
                 if (rest) {
@@ -405,8 +413,8 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
 #pragma unroll
                     for (int j = 0; j < 4; ++j) d[j] = make_uint2(bf2_mul(d[j].x, r), bf2_mul(d[j].y, r));
                 }
-                store_shared16(dst + i * 2048 + x0, d[0].x, d[0].y, d[1].x, d[1].y);
-                store_shared16(dst + i * 2048 + (x0 ^ 16), d[2].x, d[2].y, d[3].x, d[3].y);
+                store_shared16(dst + i * apart * 128 + x0, d[0].x, d[0].y, d[1].x, d[1].y);
+                store_shared16(dst + i * apart * 128 + (x0 ^ 16), d[2].x, d[2].y, d[3].x, d[3].y);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -529,7 +537,7 @@ struct PackedReduce {
     float* dw;
     long long ws_k, ws_c;
     float alpha;
-    int c, k, side, tiles_c, full, splits, log_g;
+    int c, k, tile_k, tile_c, tiles_c, full, splits, log_g;
 };
 __global__ void __launch_bounds__(256)
 packed_reduce_kernel(const __grid_constant__ PackedReduce R)
@@ -538,14 +546,14 @@ packed_reduce_kernel(const __grid_constant__ PackedReduce R)
     pdl_release_next_grid();
     const int G = 1 << R.log_g, per = 256 >> R.log_g, pos = threadIdx.x & (per - 1), g = threadIdx.x / per;
     const int tile = R.full + blockIdx.y, tk = tile / R.tiles_c, tc = tile - tk * R.tiles_c;
-    const int quads = R.side >> 2, p = blockIdx.x * per + pos, row = p / quads, q = p - row * quads;
-    const int k = tk * R.side + row, c = tc * R.side + 4 * q;
+    const int quads = R.tile_c >> 2, p = blockIdx.x * per + pos, row = p / quads, q = p - row * quads;
+    const int k = tk * R.tile_k + row, c = tc * R.tile_c + 4 * q;
     const bool in = k < R.k && c < R.c;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     pdl_wait_prior_grid();
     if (in) {
-        const size_t block = (size_t)R.side * R.side;
-        const float* src = R.partial + (size_t)blockIdx.y * R.splits * block + (size_t)row * R.side + 4 * q;
+        const size_t block = (size_t)R.tile_k * R.tile_c;
+        const float* src = R.partial + (size_t)blockIdx.y * R.splits * block + (size_t)row * R.tile_c + 4 * q;
 #pragma unroll 4
         for (int s = g; s < R.splits; s += G) {
             const float4 v = __ldcg(reinterpret_cast<const float4*>(src + s * block));
@@ -574,24 +582,24 @@ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 int round_up(int v, int m) { return (v + m - 1) / m * m; }
 
-struct PackedHost { int cg, f32, pack, npqk, full, splits, units, grid, chunks, tiles_c, tail; };
+struct PackedHost { int cg, xc, f32, pack, npqk, full, splits, units, grid, chunks, tiles_c, tail; };
 static_assert(sizeof(PackedHost) <= sizeof(((PackedPlan*)nullptr)->opaque), "opaque");
 
-template <int CG, int PLANES>
+template <int CG, int PLANES, int XC>
 cudaError_t launch(const CUtensorMap& map_dy, const CUtensorMap& map_x, const PackedParams& P, int format, int grid, cudaStream_t stream)
 {
-    auto kern = format == GACONV_ACT_E4M3 ? packed_dw_kernel<CG, PLANES, GACONV_ACT_E4M3> : packed_dw_kernel<CG, PLANES, GACONV_ACT_INT8>;
+    auto kern = format == GACONV_ACT_E4M3 ? packed_dw_kernel<CG, PLANES, XC, GACONV_ACT_E4M3> : packed_dw_kernel<CG, PLANES, XC, GACONV_ACT_INT8>;
     static std::atomic<unsigned long long> ready[2];
     const cudaError_t err = allow_shared_memory((const void*)kern, ready[format]);
     if (err != cudaSuccess) return err;
-    return launch_kernel(kern, dim3((unsigned)grid), dim3(kThreads), (size_t)Config<CG, PLANES>::bytes + 1024, stream, dim3(CG, 1, 1), map_dy, map_x, P);
+    return launch_kernel(kern, dim3((unsigned)grid), dim3(kThreads), (size_t)Config<CG, PLANES, XC>::bytes + 1024, stream, dim3(CG, 1, 1), map_dy, map_x, P);
 }
 
 }  // namespace
 
-// Tiles of 256 x 256 by CTA pairs where they leave the GPU less idle than tiles of 128 x 128, splits where tiles are few.
+// The tiles that are estimated to be quickest, and splits where they are few.
 // The estimate counts cycles: stages, and what a round, a split and a packing pass cost beside them (us, measured / estimated at 1.9 GHz: 512 rows 512->512
-// 8.5 / 8.1, 8192 rows 1024->4096 58.6 / 56, 4099 rows 1000->1333 27.8 / 28, 131072 rows 64->64 14.5 / 14.7).
+// 6.9 / 6.9, 8192 rows 1024->4096 58.6 / 56, 4099 rows 1000->1333 27.7 / 28, 131072 rows 64->64 13.4 / 14).
 bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycles)
 {
     if (g.r != 1 || g.s != 1 || g.stride_h != 1 || g.stride_w != 1 || g.pad_h != 0 || g.pad_w != 0) return false;
@@ -603,25 +611,29 @@ bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycles)
     const bool last = dy_npqk || g.k == 1 || g.p * g.q == 1;
     const bool pack = !g.bf16 || g.k % 8 != 0 || !last;
     if (pack && rows * round_up(g.k, 8) > 0x7fffffffll) return false;
-    for (int cg = 1; cg <= 2; ++cg) {
+    const int variants[3][2] = {{1, 64}, {1, 128}, {2, 128}};          // CTAs of a tile, channels of each
+    for (const auto& v : variants) {
+        const int cg = v[0], tile_k = 128 * cg, tile_c = v[1] * cg;
         PackedHost H{};
-        H.cg = cg; H.f32 = !g.bf16; H.pack = pack; H.npqk = last;
-        const int stage_rows = g.bf16 ? Config<1, 1>::rows : Config<1, 3>::rows;
+        H.cg = cg; H.xc = v[1]; H.f32 = !g.bf16; H.pack = pack; H.npqk = last;
+        const int stage_rows = g.bf16 ? kStageRows<1> : kStageRows<3>;
         H.chunks = (int)((rows + stage_rows - 1) / stage_rows);
-        H.tiles_c = ceil_div(g.c, 128 * cg);
-        const long long tiles = (long long)H.tiles_c * ceil_div(g.k, 128 * cg);
+        H.tiles_c = ceil_div(g.c, tile_c);
+        const long long tiles = (long long)H.tiles_c * ceil_div(g.k, tile_k);
         if (tiles > 1 << 24) continue;
         const int clusters = std::max(1, sms / cg);
-        const double stage = H.f32 ? (cg == 2 ? 2000 : 1600) : cg == 2 ? 1450 : 1100, fixed = 7500, block = 128.0 * 128 * cg * 4 / 20;
+        const double fixed = 7500, block = 128.0 * tile_c * 4 / 20;
         H.full = (int)(tiles / clusters * clusters);
         const int tail = (int)(tiles - H.full);
         for (int r = 0; r <= 4; ++r) {          // no split, or as many as give the tail r rounds
             const int s = r == 0 || tail == 0 ? 1 : std::min(H.chunks, r * clusters / tail);
             if (s < 1 || (r > 0 && s == 1)) continue;
-            const double rounds = std::ceil((double)tail * s / clusters);
+            const double rounds = std::ceil((double)tail * s / clusters), busy = std::min(1.0, (H.full + (double)tail * s) / clusters);
+            // (narrow tiles load as much of dY for half the work: what L2 gives when every SM asks)
+            const double stage = H.f32 ? (cg == 2 ? 2000 : v[1] == 128 ? 1600 : 1200 + 300 * busy) : cg == 2 ? 1450 : v[1] == 128 ? 1100 : 850 + 300 * busy;
             double cost = (double)(H.full / clusters) * H.chunks * stage + rounds * (ceil_div(H.chunks, s) * stage + 600) + fixed + block;
             if (pack) cost += 3000 + (double)rows * g.k * (g.bf16 ? 4 : 10) / 2600;
-            if (s > 1) cost += 5500 + (double)tail * s * 128 * 128 * cg * cg * 4 / (clusters * cg) / 20;
+            if (s > 1) cost += 5500 + (double)tail * s * tile_k * tile_c * 4 / (clusters * cg) / 20;
             if (best.units != 0 && cost >= best_cost) continue;
             best_cost = cost;
             H.splits = s; H.tail = tail;
@@ -631,7 +643,7 @@ bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycles)
         }
     }
     if (best.units == 0) return false;
-    plan->partial_bytes = best.splits == 1 ? 0 : align_up((size_t)best.tail * best.splits * (128 * best.cg) * (128 * best.cg) * sizeof(float) + 256, 256);
+    plan->partial_bytes = best.splits == 1 ? 0 : align_up((size_t)best.tail * best.splits * (128 * best.cg) * (best.xc * best.cg) * sizeof(float) + 256, 256);
     plan->dy_bytes = pack ? align_up((size_t)rows * round_up(g.k, 8) * (g.bf16 ? 2 : 6), 256) : 0;
     plan->fma = false;
     *cycles = best_cost;
@@ -657,7 +669,7 @@ cudaError_t launch_packed(const void* codes, const void* scales, int format, con
         dy = dy_scratch;
     }
     auto encode = [&](CUtensorMap* map, CUtensorMapDataType type, const void* at, int ch, size_t pitch, int third, cuuint32_t box_ch, CUtensorMapSwizzle swz) {
-        const cuuint32_t stage_rows = H.f32 ? Config<1, 3>::rows : Config<1, 1>::rows;
+        const cuuint32_t stage_rows = H.f32 ? kStageRows<3> : kStageRows<1>;
         const cuuint64_t dims[3] = {(cuuint64_t)ch, (cuuint64_t)P.rows, (cuuint64_t)third}, strides[2] = {pitch, third > 1 ? pitch * P.rows : pitch};
         const cuuint32_t box[3] = {box_ch, stage_rows, 1}, es[3] = {1, 1, 1};
         return encode_fn()(map, type, 3, const_cast<void*>(at), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -665,16 +677,16 @@ cudaError_t launch_packed(const void* codes, const void* scales, int format, con
     };
     CUtensorMap map_dy, map_x;
     if (!encode(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, g.k, (size_t)kp * 2, planes, 64, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !encode(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, act_pitch(g.c), act_pitch(g.c), 1, 128, CU_TENSOR_MAP_SWIZZLE_NONE))
+        !encode(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, act_pitch(g.c), act_pitch(g.c), 1, (cuuint32_t)H.xc, CU_TENSOR_MAP_SWIZZLE_NONE))
         return cudaErrorInvalidValue;
-    err = H.f32 ? (H.cg == 2 ? launch<2, 3>(map_dy, map_x, P, format, H.grid, stream) : launch<1, 3>(map_dy, map_x, P, format, H.grid, stream)) : H.cg == 2 ? launch<2, 1>(map_dy, map_x, P, format, H.grid, stream)
-                : launch<1, 1>(map_dy, map_x, P, format, H.grid, stream);
+    const auto run = [&](auto* bf16, auto* f32) { return (H.f32 ? f32 : bf16)(map_dy, map_x, P, format, H.grid, stream); };
+    err = H.cg == 2 ? run(launch<2, 1, 128>, launch<2, 3, 128>) : H.xc == 128 ? run(launch<1, 1, 128>, launch<1, 3, 128>) : run(launch<1, 1, 64>, launch<1, 3, 64>);
     if (err != cudaSuccess) return err;
     note_launch();
     if (H.splits == 1) return cudaSuccess;
-    PackedReduce R{partial, dw, g.ws_k, g.ws_c, g.alpha, g.c, g.k, 128 * H.cg, H.tiles_c, H.full, H.splits, 0};
+    PackedReduce R{partial, dw, g.ws_k, g.ws_c, g.alpha, g.c, g.k, 128 * H.cg, H.xc * H.cg, H.tiles_c, H.full, H.splits, 0};
     while (R.log_g < 5 && 4 << R.log_g < H.splits) ++R.log_g;
-    const int quads = R.side * R.side / 4, per = 256 >> R.log_g;
+    const int quads = R.tile_k * R.tile_c / 4, per = 256 >> R.log_g;
     err = launch_kernel(packed_reduce_kernel, dim3((unsigned)(quads / per), (unsigned)H.tail), dim3(256), 0, stream, dim3(1, 1, 1), R);
     if (err == cudaSuccess) note_launch();
     return err;
