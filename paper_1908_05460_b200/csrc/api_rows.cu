@@ -1,5 +1,7 @@
 // C-ABI entry points for rows of activations: their 8-bit form, filter gradients from it, and the root-mean-square norm.
 #include <algorithm>
+#include <cstring>
+#include <mutex>
 
 #include "gaconv_internal.h"
 
@@ -34,6 +36,37 @@ NormRows norm_rows(const gaconv_rows_desc_t& d)
 }
 size_t norm_workspace(const NormRows& o) { return std::max<size_t>(256, align_up(sizeof(float) * (size_t)norm_partials(o) * o.cols, 256)); }
 
+// Plan of a linear layer's filter gradient, the quicker of the two kernels' by their estimates.  Plans are kept, by what they depend on (2 us a call otherwise).
+struct PlanEntry { long long key[10]; bool used, ok; PackedPlan plan; };
+bool plan_linear(const Geom& g, bool npqk, bool tensor_only, PackedPlan* out)
+{
+    int dev = 0;
+    cudaGetDevice(&dev);
+    const long long key[10] = {g.n, (long long)g.p * g.q, g.c, g.k, npqk, tensor_only, g.bf16, g.sm_budget, dev,
+                               g.r != 1 || g.s != 1 || g.stride_h != 1 || g.stride_w != 1 || g.pad_h != 0 || g.pad_w != 0};
+    if (key[9]) return false;
+    unsigned long long h = 0;
+    for (long long v : key) h = (h ^ (unsigned long long)v) * 0x9E3779B97F4A7C15ull;
+    static PlanEntry table[256];
+    static std::mutex lock;
+    PlanEntry& e = table[h >> 56];
+    {
+        std::lock_guard<std::mutex> held(lock);
+        if (e.used && memcmp(e.key, key, sizeof(key)) == 0) { *out = e.plan; return e.ok; }
+    }
+    PlanEntry made{};
+    memcpy(made.key, key, sizeof(key));
+    double tensor = 0, fma = 0;
+    PackedPlan other;
+    made.used = true;
+    made.ok = plan_packed(g, npqk, &made.plan, &tensor);
+    if (!tensor_only && plan_packed_fma(g, npqk, &other, &fma) && (!made.ok || fma < tensor)) { made.plan = other; made.ok = true; }
+    std::lock_guard<std::mutex> held(lock);
+    e = made;
+    *out = made.plan;
+    return made.ok;
+}
+
 // Scratch of a filter gradient from the 8-bit form: the sums of the kernel for linear layers, or what the call on a plain X takes and X itself behind it
 struct PackedLayout { size_t inner, total; bool reads, fused; PackedPlan plan; };
 gaconv_status_t packed_layout(const gaconv_conv_desc_t* desc, int32_t method, Geom* g, PackedLayout* L)
@@ -44,13 +77,8 @@ gaconv_status_t packed_layout(const gaconv_conv_desc_t* desc, int32_t method, Ge
     L->fused = false;
     L->reads = method != GACONV_METHOD_ZERO && method != GACONV_METHOD_RANDOM;
     // (ALGO_DIRECT and the one-pass TF32 mode name kernels of the plain form)
-    if (method == GACONV_METHOD_EXACT && desc->algo != GACONV_ALGO_DIRECT && desc->math == GACONV_MATH_DEFAULT) {
-        const bool npqk = desc->dy_layout == GACONV_DY_NPQK;
-        double tensor = 0, fma = 0;
-        PackedPlan other;
-        L->fused = plan_packed(*g, npqk, &L->plan, &tensor);
-        if (plan_packed_fma(*g, npqk, &other, &fma) && desc->algo != GACONV_ALGO_TENSOR && (!L->fused || fma < tensor)) { L->plan = other; L->fused = true; }
-    }
+    if (method == GACONV_METHOD_EXACT && desc->algo != GACONV_ALGO_DIRECT && desc->math == GACONV_MATH_DEFAULT)
+        L->fused = plan_linear(*g, desc->dy_layout == GACONV_DY_NPQK, desc->algo == GACONV_ALGO_TENSOR, &L->plan);
     if (L->fused) { L->inner = 0; L->total = align_up(kWsDataOffset, 256) + L->plan.partial_bytes + L->plan.dy_bytes; return GACONV_OK; }
     if ((st = method_workspace(desc, method, kNoLimit, &L->inner)) != GACONV_OK) return st;
     L->inner = align_up(L->inner, 256);
