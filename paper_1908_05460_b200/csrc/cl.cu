@@ -63,6 +63,7 @@
 #include <cstring>
 #include <type_traits>
 
+#include "device_utils.cuh"
 #include "gaconv_internal.h"
 #include "tma.cuh"
 #include "umma.cuh"
@@ -721,19 +722,6 @@ struct PackOp {
     size_t plane;               // elements of a destination plane
 };
 
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
-    const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&t);
-}
-// two fp32 values -> their planes, packed pairwise: x0 = the upper 16 bits of x (no rounding, so nothing overflows),
-// x1 = bf16(x - x0), x2 = bf16(x - x0 - x1); both differences are exact
-__device__ __forceinline__ void split2(float u, float v, uint32_t (&w)[3]) {
-    const uint32_t a = __float_as_uint(u) & 0xffff0000u, b = __float_as_uint(v) & 0xffff0000u;
-    w[0] = (a >> 16) | b;
-    const float ru = u - __uint_as_float(a), rv = v - __uint_as_float(b);
-    w[1] = bf16_pair(ru, rv);
-    w[2] = bf16_pair(ru - __uint_as_float(w[1] << 16), rv - __uint_as_float(w[1] & 0xffff0000u));
-}
 // copies the first n <= 16 bytes of a 16-byte piece to shared memory without a stop in registers; zeros behind them
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int n) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");

@@ -40,4 +40,18 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&t);
+}
+// two fp32 values -> their planes, packed pairwise: x0 = the upper 16 bits of x (no rounding, so nothing overflows),
+// x1 = bf16(x - x0), x2 = bf16(x - x0 - x1); both differences are exact
+__device__ __forceinline__ void split2(float u, float v, uint32_t (&w)[3]) {
+    const uint32_t a = __float_as_uint(u) & 0xffff0000u, b = __float_as_uint(v) & 0xffff0000u;
+    w[0] = (a >> 16) | b;
+    const float ru = u - __uint_as_float(a), rv = v - __uint_as_float(b);
+    w[1] = bf16_pair(ru, rv);
+    w[2] = bf16_pair(ru - __uint_as_float(w[1] << 16), rv - __uint_as_float(w[1] & 0xffff0000u));
+}
+
 }  // namespace gaconv

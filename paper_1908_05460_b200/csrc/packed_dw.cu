@@ -6,8 +6,13 @@
 // So X goes from memory to the SM in 8 bits, is turned into bf16 on the way from one piece of shared memory to another, and lies there in the
 // order that the tensor core reads: half the bytes of a bf16 X and no copy of it in memory.  dY is the M side, X the N side, both MN-major (a row of
 // shared memory is a row t, 64 channels of it); fp32 gradients are three bf16 planes dY = d0 + d1 + d2 (8 + 8 + 8 bits) whose products add up
-// in the same accumulators.  Gradients that the copy engine cannot read as they lie (fp32, another order, a number of outputs that is no
-// multiple of 8) are packed into the workspace first.
+// in the same accumulators.  Gradients that the copy engine cannot read as they lie (another order, rows that do not start on 16 bytes) are packed
+// into the workspace first, fp32 ones as planes.
+//
+// fp32 gradients that it can read are split into planes by the threads that turn X, beside it (RAW).  For 64 rows 240 KB then pass through an SM's shared
+// memory (128 bytes a cycle), and a stage takes 2300 cycles where one of packed planes takes 1600 (pairs: 2750, 2000); but no pass over dY comes
+// first.  us, split inside and packed first: 4096 rows 512 -> 512 19.2, 21.8; 65536 rows 256 -> 256 37, 58; 131072 rows 64 -> 64 24.0, 29.8; 16384
+// rows 1024 -> 1024 98, 97; 16384 rows 2048 -> 256 53.6, 48.2; 16384 rows 4096 -> 1024 352, 281.
 //
 // A CTA pair (CG = 2) shares a tile of 256 x 256: each CTA holds 128 outputs of dY and 128 channels of X, and the pair's MMAs read both halves of X,
 // so that a turned element serves 256 outputs.  CG = 1: tiles of 128 x 128, or 128 x 64, for problems that would not fill the GPU with larger ones (us by
@@ -36,6 +41,7 @@
 #include <cstring>
 
 #include "act8.cuh"
+#include "device_utils.cuh"
 #include "gaconv_internal.h"
 #include "tma.cuh"
 #include "umma.cuh"
@@ -51,9 +57,13 @@ constexpr int kMaxRing = 4;
 // Three rings: dY and X in 8 bits as they are copied, `halves` x 64 rows at a time (a warp takes ~500 cycles for its round of wait, byte count and copy, however
 // large the copy is, and the MMAs 512 for 64 rows), and X turned, 64 rows at a time.
 template <int PLANES> constexpr int kStageRows = PLANES == 3 ? kRows : 2 * kRows;
-template <int CG, int PLANES, int XC> struct Config {           // XC: channels of X that a CTA turns
+// XC: channels of X that a CTA turns.  RAW: fp32 gradients as they lie, split into planes beside it.
+template <int CG, int PLANES, int XC, bool RAW> struct Config {
+    static_assert(!RAW || PLANES == 3, "fp32");
     static constexpr int cols = XC * CG, halves = PLANES == 3 ? 1 : 2, rows = kStageRows<PLANES>, atoms = XC / 64;
-    static constexpr int dy_stage = 2 * PLANES * halves * kTile, dys = 3, turned = atoms * kTile, turneds = PLANES == 3 ? 2 : 4, raws = PLANES == 3 ? 4 : 3;
+    static constexpr int split = RAW ? 2 * PLANES * kTile : 0;      // bytes of dY in a slot of what is turned
+    static constexpr int dy_stage = RAW ? kRows * 128 * 4 : 2 * PLANES * halves * kTile, dys = RAW ? 2 : 3;
+    static constexpr int turned = split + atoms * kTile, turneds = PLANES == 3 ? 2 : 4, raws = RAW ? 2 : PLANES == 3 ? 4 : 3;
     static constexpr int raw = rows * XC + rows * 8;                // the channels in 8 bits, and the two words around the scales of each row
     static constexpr int turned_at = dys * dy_stage, raw_at = turned_at + turneds * turned, out_at = raw_at + raws * raw, bytes = out_at + 8 * 1024;
     static constexpr int epoch = PLANES == 3 ? 4 : 8;               // stages of dY: chains of 48 or 64 MMAs
@@ -61,7 +71,7 @@ template <int CG, int PLANES, int XC> struct Config {           // XC: channels 
     static constexpr int regs_control = 48, regs_turn = CG == 2 ? 56 : 80, regs_sum = CG == 2 ? 160 : 104;
     static_assert(4 * regs_control + 8 * regs_turn + 8 * regs_sum <= 20 * 96, "registers");
     // A wait for a phase is only right once the phase before is over, which a group knows of its own stages alone: no slot passes from one group to the other
-    static_assert(turneds % 2 == 0 && raws * halves % 2 == 0, "two groups turn X");
+    static_assert(turneds % 2 == 0 && raws * halves % 2 == 0 && (!RAW || dys == 2), "two groups turn X");
     static_assert(dys <= kMaxRing && turneds <= kMaxRing && raws <= kMaxRing && bytes <= 225 * 1024 && raw % 128 == 0, "shared memory");
 };
 
@@ -166,11 +176,11 @@ struct Walk {
     }
 };
 
-template <int CG, int PLANES, int XC, int FMT>
+template <int CG, int PLANES, int XC, bool RAW, int FMT>
 __global__ void __launch_bounds__(kThreads, 1)
 packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ PackedParams P)
 {
-    typedef Config<CG, PLANES, XC> C;
+    typedef Config<CG, PLANES, XC, RAW> C;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_dy[kMaxRing], bar_free_dy[kMaxRing], bar_full[kMaxRing], bar_empty[kMaxRing], bar_raw[kMaxRing], bar_taken[kMaxRing], bar_acc[2], bar_free[2], bar_last;
     __shared__ uint32_t s_tmem;
@@ -181,7 +191,7 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
 
     pdl_release_next_grid();
     if (threadIdx.x == 0) {
-        for (int i = 0; i < C::dys; ++i) { mbar_init(smem_u32(&bar_dy[i]), rank == 0 ? CG : 1); mbar_init(smem_u32(&bar_free_dy[i]), 1); }
+        for (int i = 0; i < C::dys; ++i) { mbar_init(smem_u32(&bar_dy[i]), rank == 0 && !RAW ? CG : 1); mbar_init(smem_u32(&bar_free_dy[i]), RAW ? 4 : 1); }
         for (int i = 0; i < C::turneds; ++i) { mbar_init(smem_u32(&bar_full[i]), 4 * CG); mbar_init(smem_u32(&bar_empty[i]), 1); }
         for (int i = 0; i < C::raws; ++i) { mbar_init(smem_u32(&bar_raw[i]), 1 + 32); mbar_init(smem_u32(&bar_taken[i]), 4 * C::halves); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bar_acc[i]), 1); mbar_init(smem_u32(&bar_free[i]), 8 * CG); }
@@ -248,7 +258,9 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
                 const uint32_t bar = smem_u32(&bar_dy[st]);
                 if (lane == 0) mbar_expect_tx(bar, C::dy_stage);
                 __syncwarp();
-                if (lane < 2 * PLANES)
+                if (RAW) {
+                    if (lane < 4) tma_load_3d(base + st * C::dy_stage + lane * kTile, &map_dy, bar, (w.k0 * CG + rank) * 128 + 32 * lane, w.chunk * C::rows, 0);
+                } else if (lane < 2 * PLANES)
                     tma_load_3d(base + st * C::dy_stage + lane * C::halves * kTile, &map_dy, bar, (w.k0 * CG + rank) * 128 + 64 * (lane & 1), w.chunk * C::rows, lane >> 1);
                 if (++st == C::dys) { st = 0; ph ^= 1; }
                 ++n;
@@ -287,7 +299,7 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
                 taken = n < C::raws || mbar_look(smem_u32(&bar_taken[st]), ph ^ 1);
             }
             if (!ok) { give_up(); asm volatile("cp.async.wait_all;" ::: "memory"); }
-        } else if (CG == 2 && warp == 1 && rank == 1) {
+        } else if (CG == 2 && !RAW && warp == 1 && rank == 1) {
             // ------------------------------------------------------------ tells the leader of this CTA's copies of dY
             Walk w;
             w.start(P, group);
@@ -312,7 +324,7 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
                 int in_epoch = 0;
                 for (int left = w.left; left > 0; --left) {
                     if (in_epoch == 0 && epochs >= 2) ok = pair_wait(smem_u32(&bar_free[set]), ((epochs >> 1) - 1) & 1);
-                    if (!ready_dy) ok = ok && pair_wait(smem_u32(&bar_dy[ds]), dph);
+                    if (!RAW && !ready_dy) ok = ok && pair_wait(smem_u32(&bar_dy[ds]), dph);
                     const int next_ds = ds + 1 == C::dys ? 0 : ds + 1;
                     dph ^= next_ds == 0 ? 1 : 0;
                     const bool ends = left == 1 || in_epoch + 1 == C::epoch;
@@ -325,9 +337,9 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
                         const int next = st + 1 == C::turneds ? 0 : st + 1;
                         ph ^= next == 0 ? 1 : 0;
                         ready = mbar_look(smem_u32(&bar_full[next]), ph);
-                        if (h == C::halves - 1) ready_dy = mbar_look(smem_u32(&bar_dy[next_ds]), dph);
+                        if (!RAW && h == C::halves - 1) ready_dy = mbar_look(smem_u32(&bar_dy[next_ds]), dph);
                         if (elect_one()) {
-                            const uint32_t a0 = base + ds * C::dy_stage + h * kTile, b0 = base + C::turned_at + st * C::turned;
+                            const uint32_t slot = base + C::turned_at + st * C::turned, a0 = RAW ? slot : base + ds * C::dy_stage + h * kTile, b0 = slot + C::split;
                             const uint64_t a = hi | (lbo_dy | (a0 >> 4)), b = hi | (lbo_x | (b0 >> 4));
                             const uint32_t d = tmem + set * C::cols;
 #pragma unroll
@@ -336,7 +348,7 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
                                 for (int pl = PLANES - 1; pl >= 0; --pl)
                                     mma<CG>(d, a + (pl * 2 * C::halves * kTile + i * 2048) / 16, b + i * 2048 / 16, idesc, in_epoch > 0 || h > 0 || i > 0 || pl < PLANES - 1 ? 1u : 0u);
                             commit<CG>(smem_u32(&bar_empty[st]));
-                            if (h == C::halves - 1) commit<CG>(smem_u32(&bar_free_dy[ds]));
+                            if (!RAW && h == C::halves - 1) commit<CG>(smem_u32(&bar_free_dy[ds]));
                             if (h == C::halves - 1 && ends) commit<CG>(smem_u32(&bar_acc[set]));
                         }
                         __syncwarp();
@@ -374,11 +386,12 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
         const uint32_t from = raw + (half + row) * XC + 16 * q;
         // (a row's first scale lies at byte (row * groups + its group) % 4 of its two words, the same for rows 4 apart)
         const uint32_t scale = raw + C::rows * XC + (half + row) * 8 + (q >> 1);
-        const uint32_t to = base + C::turned_at + (q >> 2) * kTile + row * 128, x0 = ((2 * (q & 3)) ^ (row & 7)) << 4;
+        const uint32_t to = base + C::turned_at + C::split + (q >> 2) * kTile + row * 128, x0 = ((2 * (q & 3)) ^ (row & 7)) << 4;
         Walk w;
         w.start(P, group);
         if (C::halves == 1 && mine == 1 && w.live()) w.next(P, step);
         int st = mine, ph = 0, rs = C::halves == 1 ? mine : 0, rph = 0, n = mine;
+        int dph = 0;
         bool ok = true, filled = false, empty = true;
         while (w.live()) {
             if (!filled) ok = mbar_wait(smem_u32(&bar_raw[rs]), rph);
@@ -416,9 +429,33 @@ packed_dw_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_consta
                 store_shared16(dst + i * apart * 128 + x0, d[0].x, d[0].y, d[1].x, d[1].y);
                 store_shared16(dst + i * apart * 128 + (x0 ^ 16), d[2].x, d[2].y, d[3].x, d[3].y);
             }
+            if constexpr (RAW) {
+                // dY: eight outputs of row t / 16 + 8 i a thread, three planes of them.  The copies come in boxes of 32 outputs, which eight lanes read two of:
+                // those of the second take their 16-byte halves in the other order, into banks that the first leave free.
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_dy[mine]), dph));
+                if (!ok) break;
+                dph ^= 1;
+                const int j = t & 15, swap = j >> 2 & 1;
+                const uint32_t src = base + mine * C::dy_stage + (j >> 2) * kTile + (t >> 4) * 128 + (j & 3) * 32;
+                const uint32_t out = base + C::turned_at + old_st * C::turned + (j >> 3) * kTile + (t >> 4) * 128 + (((j & 7) ^ (t >> 4 & 7)) << 4);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint4 a = load_shared16(src + i * 1024 + 16 * swap), b = load_shared16(src + i * 1024 + 16 * (swap ^ 1));
+                    const uint4 lo = swap ? b : a, hi = swap ? a : b;
+                    uint32_t p0[3], p1[3], p2[3], p3[3];
+                    split2(__uint_as_float(lo.x), __uint_as_float(lo.y), p0); split2(__uint_as_float(lo.z), __uint_as_float(lo.w), p1);
+                    split2(__uint_as_float(hi.x), __uint_as_float(hi.y), p2); split2(__uint_as_float(hi.z), __uint_as_float(hi.w), p3);
+#pragma unroll
+                    for (int pl = 0; pl < 3; ++pl) store_shared16(out + pl * 2 * kTile + i * 1024, p0[pl], p1[pl], p2[pl], p3[pl]);
+                }
+            }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            if (lane == 0) { arrive_leader<CG>(smem_u32(&bar_full[old_st])); arrive(smem_u32(&bar_taken[old_rs])); }
+            if (lane == 0) {
+                arrive_leader<CG>(smem_u32(&bar_full[old_st]));
+                arrive(smem_u32(&bar_taken[old_rs]));
+                if (RAW) arrive(smem_u32(&bar_free_dy[mine]));
+            }
             w.next(P, step);
             if (C::halves == 1 && w.live()) w.next(P, step);
         }
@@ -582,17 +619,17 @@ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 int round_up(int v, int m) { return (v + m - 1) / m * m; }
 
-struct PackedHost { int cg, xc, f32, pack, npqk, full, splits, units, grid, chunks, tiles_c, tail; };
+struct PackedHost { int cg, xc, f32, raw, pack, npqk, full, splits, units, grid, chunks, tiles_c, tail; };
 static_assert(sizeof(PackedHost) <= sizeof(((PackedPlan*)nullptr)->opaque), "opaque");
 
-template <int CG, int PLANES, int XC>
+template <int CG, int PLANES, int XC, bool RAW>
 cudaError_t launch(const CUtensorMap& map_dy, const CUtensorMap& map_x, const PackedParams& P, int format, int grid, cudaStream_t stream)
 {
-    auto kern = format == GACONV_ACT_E4M3 ? packed_dw_kernel<CG, PLANES, XC, GACONV_ACT_E4M3> : packed_dw_kernel<CG, PLANES, XC, GACONV_ACT_INT8>;
+    auto kern = format == GACONV_ACT_E4M3 ? packed_dw_kernel<CG, PLANES, XC, RAW, GACONV_ACT_E4M3> : packed_dw_kernel<CG, PLANES, XC, RAW, GACONV_ACT_INT8>;
     static std::atomic<unsigned long long> ready[2];
     const cudaError_t err = allow_shared_memory((const void*)kern, ready[format]);
     if (err != cudaSuccess) return err;
-    return launch_kernel(kern, dim3((unsigned)grid), dim3(kThreads), (size_t)Config<CG, PLANES, XC>::bytes + 1024, stream, dim3(CG, 1, 1), map_dy, map_x, P);
+    return launch_kernel(kern, dim3((unsigned)grid), dim3(kThreads), (size_t)Config<CG, PLANES, XC, RAW>::bytes + 1024, stream, dim3(CG, 1, 1), map_dy, map_x, P);
 }
 
 }  // namespace
@@ -609,20 +646,21 @@ bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycles)
     double best_cost = 0;
     const int sms = g.sm_budget > 0 ? std::min(g.sm_budget, device_sms()) : device_sms();
     const bool last = dy_npqk || g.k == 1 || g.p * g.q == 1;
-    const bool pack = !g.bf16 || g.k % 8 != 0 || !last;
-    if (pack && rows * round_up(g.k, 8) > 0x7fffffffll) return false;
-    const int variants[3][2] = {{1, 64}, {1, 128}, {2, 128}};          // CTAs of a tile, channels of each
+    const bool raw_fits = !g.bf16 && last && g.k % 4 == 0;          // fp32 rows that the copy engine can read
+    const int variants[6][3] = {{1, 64, 0}, {1, 128, 0}, {2, 128, 0}, {1, 64, 1}, {1, 128, 1}, {2, 128, 1}};          // CTAs of a tile, channels of each, fp32 split inside
     for (const auto& v : variants) {
         const int cg = v[0], tile_k = 128 * cg, tile_c = v[1] * cg;
+        const bool raw = v[2] != 0, pack = !raw && (!g.bf16 || g.k % 8 != 0 || !last);
+        if ((raw && !raw_fits) || (pack && rows * round_up(g.k, 8) > 0x7fffffffll)) continue;
         PackedHost H{};
-        H.cg = cg; H.xc = v[1]; H.f32 = !g.bf16; H.pack = pack; H.npqk = last;
+        H.cg = cg; H.xc = v[1]; H.f32 = !g.bf16; H.raw = raw; H.pack = pack; H.npqk = last;
         const int stage_rows = g.bf16 ? kStageRows<1> : kStageRows<3>;
         H.chunks = (int)((rows + stage_rows - 1) / stage_rows);
         H.tiles_c = ceil_div(g.c, tile_c);
         const long long tiles = (long long)H.tiles_c * ceil_div(g.k, tile_k);
         if (tiles > 1 << 24) continue;
         const int clusters = std::max(1, sms / cg);
-        const double fixed = 7500, block = 128.0 * tile_c * 4 / 20;
+        const double fixed = raw && cg == 1 ? 5000 : 7500, block = 128.0 * tile_c * 4 / 20;
         H.full = (int)(tiles / clusters * clusters);
         const int tail = (int)(tiles - H.full);
         for (int r = 0; r <= 4; ++r) {          // no split, or as many as give the tail r rounds
@@ -630,9 +668,11 @@ bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycles)
             if (s < 1 || (r > 0 && s == 1)) continue;
             const double rounds = std::ceil((double)tail * s / clusters), busy = std::min(1.0, (H.full + (double)tail * s) / clusters);
             // (narrow tiles load as much of dY for half the work: what L2 gives when every SM asks)
-            const double stage = H.f32 ? (cg == 2 ? 2000 : v[1] == 128 ? 1600 : 1200 + 300 * busy) : cg == 2 ? 1450 : v[1] == 128 ? 1100 : 850 + 300 * busy;
+            const double stage = raw ? (cg == 2 ? 2750 : v[1] == 128 ? 2300 : 2100)
+                               : H.f32 ? (cg == 2 ? 2000 : v[1] == 128 ? 1600 : 1200 + 300 * busy)
+                               : cg == 2 ? 1450 : v[1] == 128 ? 1100 : 850 + 300 * busy;
             double cost = (double)(H.full / clusters) * H.chunks * stage + rounds * (ceil_div(H.chunks, s) * stage + 600) + fixed + block;
-            if (pack) cost += 3000 + (double)rows * g.k * (g.bf16 ? 4 : 10) / 2600;
+            if (pack) cost += 3000 + (double)rows * g.k * (g.bf16 ? 4.0 / 2600 : 10.0 / 3600);
             if (s > 1) cost += 5500 + (double)tail * s * tile_k * tile_c * 4 / (clusters * cg) / 20;
             if (best.units != 0 && cost >= best_cost) continue;
             best_cost = cost;
@@ -644,7 +684,7 @@ bool plan_packed(const Geom& g, bool dy_npqk, PackedPlan* plan, double* cycles)
     }
     if (best.units == 0) return false;
     plan->partial_bytes = best.splits == 1 ? 0 : align_up((size_t)best.tail * best.splits * (128 * best.cg) * (best.xc * best.cg) * sizeof(float) + 256, 256);
-    plan->dy_bytes = pack ? align_up((size_t)rows * round_up(g.k, 8) * (g.bf16 ? 2 : 6), 256) : 0;
+    plan->dy_bytes = best.pack ? align_up((size_t)rows * round_up(g.k, 8) * (g.bf16 ? 2 : 6), 256) : 0;
     plan->fma = false;
     *cycles = best_cost;
     memcpy(plan->opaque, &best, sizeof(best));
@@ -676,11 +716,14 @@ cudaError_t launch_packed(const void* codes, const void* scales, int format, con
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
     };
     CUtensorMap map_dy, map_x;
-    if (!encode(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, g.k, (size_t)kp * 2, planes, 64, CU_TENSOR_MAP_SWIZZLE_128B) ||
+    if (!(H.raw ? encode(&map_dy, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, dy, g.k, (size_t)g.k * 4, 1, 32, CU_TENSOR_MAP_SWIZZLE_NONE)
+                : encode(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dy, g.k, (size_t)kp * 2, planes, 64, CU_TENSOR_MAP_SWIZZLE_128B)) ||
         !encode(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, act_pitch(g.c), act_pitch(g.c), 1, (cuuint32_t)H.xc, CU_TENSOR_MAP_SWIZZLE_NONE))
         return cudaErrorInvalidValue;
-    const auto run = [&](auto* bf16, auto* f32) { return (H.f32 ? f32 : bf16)(map_dy, map_x, P, format, H.grid, stream); };
-    err = H.cg == 2 ? run(launch<2, 1, 128>, launch<2, 3, 128>) : H.xc == 128 ? run(launch<1, 1, 128>, launch<1, 3, 128>) : run(launch<1, 1, 64>, launch<1, 3, 64>);
+    const auto run = [&](auto* bf16, auto* f32, auto* raw) { return (H.raw ? raw : H.f32 ? f32 : bf16)(map_dy, map_x, P, format, H.grid, stream); };
+    err = H.cg == 2 ? run(launch<2, 1, 128, false>, launch<2, 3, 128, false>, launch<2, 3, 128, true>)
+        : H.xc == 128 ? run(launch<1, 1, 128, false>, launch<1, 3, 128, false>, launch<1, 3, 128, true>)
+                      : run(launch<1, 1, 64, false>, launch<1, 3, 64, false>, launch<1, 3, 64, true>);
     if (err != cudaSuccess) return err;
     note_launch();
     if (H.splits == 1) return cudaSuccess;

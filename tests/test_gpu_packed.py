@@ -195,6 +195,36 @@ def test_linear_of_many_tiles(m, c, k, dtype):
     Case(linear(m, c, k), dtype, B.ACT_INT8 if m % 2 else B.ACT_E4M3).check()
 
 
+# fp32 gradients in rows of 16 bytes, which are split into bf16 planes inside the kernel: tiles of 64 and of 128 channels, pairs; a last tile of four outputs;
+# few rows, rows that end inside a stage, an odd number of stages a split; and rows of dY that do not start on 16 bytes beside them
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("m, c, k", [(20000, 64, 64), (200, 700, 700), (1000, 1000, 1000), (4097, 300, 516), (2048, 128, 1000), (33, 1400, 1300), (65, 2100, 1156), (2111, 515, 2052),
+                                     (30001, 256, 260), (4097, 300, 518), (33, 1400, 1301)])
+def test_linear_fp32_gradients(m, c, k, fmt):
+    Case(linear(m, c, k), torch.float32, fmt).check()
+
+
+@pytest.mark.parametrize("m, c, k", [(1000, 200, 400), (4097, 300, 516), (30001, 256, 260), (4097, 300, 518)])
+def test_fp32_gradients_of_every_magnitude(m, c, k):
+    """Outputs whose gradients lie far apart; an Inf and a NaN stay in the output that they belong to, and zeros are zeros."""
+    case = Case(linear(m, c, k), torch.float32, B.ACT_E4M3)
+    dy = case.dy.reshape(m, k)
+    dy[:, 0] *= 1e-28
+    dy[:, 1] *= 1e30
+    dy[:, 2] = 0.0
+    dy[m - 1, 4] = float("inf")
+    dy[m // 2, k - 1] = float("nan")
+    case.dy64 = R.f64(dy).reshape(m, k, 1, 1)
+    case.run()
+    d = case.result()[1][:, :, 0, 0]
+    assert not np.isfinite(d[4]).any() and not np.isfinite(d[k - 1]).any()
+    assert (d[2] == 0).all()
+    case.dy64 = np.nan_to_num(case.dy64, nan=0.0, posinf=0.0)
+    want, size = case.reference()
+    rest = [i for i in range(k) if i not in (4, k - 1)]
+    assert norm_err(d[rest], want[rest, :, 0, 0], size[rest, :, 0, 0]) <= TOL
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_linear_transposed_result_of_many_tiles(dtype):
     Case(linear(700, 1300, 1100), dtype, B.ACT_E4M3, dw_layout=B.DW_RSCK, alpha=0.5).check()
