@@ -6,7 +6,6 @@
 //            Nothing has to be put together, as long as every tensor of a call has the same boundaries (strides that are alike modulo N).
 //   columns  pieces of the row (what a group of an 8-bit scale needs); one is put together from the two pieces of memory that it straddles, and
 //            written as the one that it shares with its neighbour, a lane up.
-// (Element by element, 2 bytes at a time, 8000 rows of 1333 bf16 took four times as long as rows of 1336.)
 //
 // No byte past the end of a tensor is read, and none outside a row is written.
 #pragma once
