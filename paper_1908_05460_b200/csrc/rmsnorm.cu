@@ -68,8 +68,11 @@ __device__ __forceinline__ uint4 load_weight(const T* __restrict__ w, int c, int
 
 // Blocks stay and their teams take rows in turn, the next one's loads on their way while a row is worked on.  Where rows are not whole pieces a team's
 // rows are a multiple of N apart: they have one frame, and the weight's pieces in it stay in registers.
-template <typename T, int NU, bool FULL>
-__global__ void __launch_bounds__(512)
+// WIDE: registers for three blocks of 256 threads an SM.  Rows of more than 128 threads gain by it, shorter ones lose (us without, with: 16384x4096 bf16 104.6,
+// 100.8; 8192x3584 bf16 51.8, 49.8; 8000x1333 fp32 56.8, 48.6; 16384x1024 bf16 28.0, 29.3; 16000x333 fp32 36.6, 40.4; without codes 16384x4096 bf16 90.7, 94.0;
+// bf16 rows that are not whole pieces 8000x3003 66.9, 69.5; few of bf16 512x4096 6.2, 6.4).
+template <typename T, int NU, bool FULL, bool WIDE = false>
+__global__ void __launch_bounds__(WIDE ? 256 : 512, WIDE ? 3 : 1)
 rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __restrict__ w, T* sum, T* y, uint8_t* codes, uint8_t* scales, float* rstd, int lanes)
 {
     constexpr int N = kPiece<T>;
@@ -402,12 +405,14 @@ cudaError_t forward(const NormRows& o, const T* x, const T* res, const T* w, T* 
         return launch_kernel(kern, dim3((unsigned)o.rows), dim3(512), 0, stream, dim3(1, 1, 1), o, x, res, w, sum, y, codes, scales, rstd);
     }
     const int teams = std::max(1, 128 / t.lanes), threads = teams * t.lanes;
+    const bool wide = t.nu == 2 && t.lanes > 128 && codes != nullptr && (sizeof(T) == 4 || (t.full && o.rows > 16ll * device_sms()));          // (two pieces: at most 256 threads)
     auto kern = t.nu == 1 ? (t.full ? rmsnorm_forward_kernel<T, 1, true> : rmsnorm_forward_kernel<T, 1, false>)
+              : wide ? (t.full ? rmsnorm_forward_kernel<T, 2, true, true> : rmsnorm_forward_kernel<T, 2, false, sizeof(T) == 4>)
               : t.nu == 2 ? (t.full ? rmsnorm_forward_kernel<T, 2, true> : rmsnorm_forward_kernel<T, 2, false>)
                           : (t.full ? rmsnorm_forward_kernel<T, 4, true> : rmsnorm_forward_kernel<T, 4, false>);
     // blocks that an SM holds, asked once per kernel, size and device (all devices of a process alike)
-    static std::atomic<int> resident[2][3][kMaxTeam / 32 + 1];
-    std::atomic<int>& known = resident[t.full][t.nu / 2][threads / 32];
+    static std::atomic<int> resident[2][4][kMaxTeam / 32 + 1];
+    std::atomic<int>& known = resident[t.full][wide ? 3 : t.nu / 2][threads / 32];
     int per_sm = known.load(std::memory_order_relaxed);
     if (per_sm == 0) {
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, threads, 0) != cudaSuccess || per_sm < 1) per_sm = 1;

@@ -107,6 +107,15 @@ def test_forward(rows, cols, dtype):
     n.check_forward()
 
 
+# many rows of more than 128 threads, whole pieces and not, more rows than teams
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows, cols", [(2500, 2600), (2500, 2603), (700, 1333), (480, 1400), (1400, 1999)])
+def test_forward_of_wide_rows(rows, cols, dtype):
+    n = Norm(rows, cols, dtype, fmt=rows % 2)
+    n.forward()
+    n.check_forward()
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("strides", [(104, 112, 128, 120), (101, 100, 102, 103), (112, 0, 0, 101)])
 def test_forward_strides(strides, dtype):
