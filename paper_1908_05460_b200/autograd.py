@@ -21,7 +21,7 @@ from torch.autograd.function import once_differentiable
 
 from . import binding as B
 from .layers import ConvLayer
-from .packed import DTYPES, PackedActivation, as_rows, check_format, row_stride
+from .packed import DTYPES, PackedActivation, as_rows, check_devices, check_format, row_stride
 
 
 class _Conv2dFilterGrad(torch.autograd.Function):
@@ -180,6 +180,7 @@ class GALinear(torch.nn.Module):
     def forward(self, x, packed: Optional[PackedActivation] = None):
         if x.dtype != self.weight.dtype or x.shape[-1] != self.weight.shape[1]:
             raise ValueError("input %s %s for a layer of %s %s" % (tuple(x.shape), x.dtype, tuple(self.weight.shape), self.weight.dtype))
+        check_devices(input=x, weight=self.weight, kept=None if packed is None else packed.codes)
         if packed is not None and (packed.rows * packed.cols != x.numel() or packed.cols != x.shape[-1] or packed.dtype != x.dtype):
             raise ValueError("the kept input has %d x %d values of %s, the input %s" % (packed.rows, packed.cols, packed.dtype, tuple(x.shape)))
         return _LinearFilterGrad.apply(x, self.weight, self.bias, packed, self.checkpoint)
@@ -244,6 +245,7 @@ class GARMSNorm(torch.nn.Module):
     def forward(self, x, residual=None) -> NormOutput:
         if x.dtype != self.weight.dtype or x.shape[-1] != self.weight.shape[0] or (residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype)):
             raise ValueError("input %s %s for a norm of %s %s, and a residual alike" % (tuple(x.shape), x.dtype, tuple(self.weight.shape), self.weight.dtype))
+        check_devices(input=x, residual=residual, weight=self.weight)
         packed = None
         if self.checkpoint is not None:
             packed = PackedActivation(x.numel() // x.shape[-1], x.shape[-1], x.dtype, self.checkpoint, x.device)

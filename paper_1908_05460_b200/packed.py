@@ -18,6 +18,13 @@ def check_format(name):
     return name
 
 
+def check_devices(**tensors):
+    """A kernel is given addresses alone, and one of another device's memory, or the host's, faults there."""
+    at = {name: t.device for name, t in tensors.items() if t is not None}
+    if len(set(at.values())) > 1:
+        raise ValueError("tensors on several devices: " + ", ".join("%s on %s" % i for i in at.items()))
+
+
 def as_rows(x: torch.Tensor) -> torch.Tensor:
     """x [..., cols] as rows that the library can read: neighbouring channels, on a 16-byte boundary."""
     if x.dtype not in DTYPES:
@@ -76,6 +83,7 @@ class PackedActivation:
 
     def filter_gradient(self, dy, dw, desc: B.ConvDesc, method: int = B.METHOD_EXACT, seed: int = 0):
         """gaconv_dw_from_packed in a workspace of this call's own; desc says what layer the rows belong to."""
+        check_devices(kept=self.codes, dy=dy, dw=dw)
         if desc.n * desc.h * desc.w != self.rows or desc.c != self.cols:
             raise ValueError("%d x %d values are kept, the layer has %d x %d" % (self.rows, self.cols, desc.n * desc.h * desc.w, desc.c))
         p = (desc.h + 2 * desc.pad_h - desc.r) // desc.stride_h + 1

@@ -1,0 +1,54 @@
+"""What the layers that keep their inputs in 8 bits hand to the library, and what they refuse: no GPU needed, the library's calls are replaced by recorders."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_1908_05460_b200 import binding as B
+from paper_1908_05460_b200 import build as build_mod
+from paper_1908_05460_b200.autograd import GALinear, GARMSNorm
+from paper_1908_05460_b200.layers import ConvLayer
+from paper_1908_05460_b200.packed import PackedActivation
+
+ENQUEUE = ["gaconv_act_pack", "gaconv_act_unpack", "gaconv_dw_from_packed", "gaconv_dw_exact", "gaconv_rmsnorm_forward", "gaconv_rmsnorm_backward", "gaconv_workspace_init"]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    build_mod.build()
+    B.load()
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The calls that would have been made, in order: (name, arguments).  "cpu" and "meta" stand for two devices."""
+    made = []
+    for name in ENQUEUE:
+        monkeypatch.setattr(B, name, lambda *a, name=name, **k: made.append((name, a)))
+    monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+    return made
+
+
+def linear_desc(rows=4, c=16, k=8):
+    return B.make_desc(ConvLayer("linear", rows, c, 1, 1, k, 1, 1), torch.bfloat16, dy_layout=B.DY_NPQK)
+
+
+def test_tensors_on_several_devices_are_refused(calls):
+    x = torch.zeros(4, 16, dtype=torch.bfloat16)
+    for norm in (GARMSNorm(16, device="cpu"), GARMSNorm(16, checkpoint="int8", device="cpu")):
+        norm(x, x)
+        assert calls.pop()[0] == "gaconv_rmsnorm_forward"
+        with pytest.raises(ValueError, match="several devices"):
+            norm(x, x.to("meta"))
+        with pytest.raises(ValueError, match="several devices"):
+            norm(x.to("meta"))
+    here, there = PackedActivation(4, 16, x.dtype, "e4m3", "cpu"), PackedActivation(4, 16, x.dtype, "e4m3", "meta")
+    layer = GALinear(16, 8, device="cpu")
+    layer(x, here)
+    with pytest.raises(ValueError, match="several devices"):
+        layer(x, there)
+    dy, dw = torch.zeros(4, 8, dtype=x.dtype), torch.zeros(8, 16)
+    for packed, dy, dw in ((there, dy, dw), (here, dy.to("meta"), dw), (here, dy, dw.to("meta"))):
+        with pytest.raises(ValueError, match="several devices"):
+            packed.filter_gradient(dy, dw, linear_desc())
+    assert not calls
