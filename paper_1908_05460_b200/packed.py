@@ -25,6 +25,16 @@ def check_devices(**tensors):
         raise ValueError("tensors on several devices: " + ", ".join("%s on %s" % i for i in at.items()))
 
 
+def is_dense(t: torch.Tensor) -> bool:
+    """Whether t's elements fill the memory from its first to its last one, each once, in whatever order."""
+    step = 1
+    for stride, size in sorted((stride, size) for size, stride in zip(t.shape, t.stride()) if size != 1):
+        if stride != step:
+            return t.numel() == 0
+        step *= size
+    return True
+
+
 def as_rows(x: torch.Tensor) -> torch.Tensor:
     """x [..., cols] as rows that the library can read: neighbouring channels, on a 16-byte boundary."""
     if x.dtype not in DTYPES:
@@ -90,6 +100,8 @@ class PackedActivation:
         q = (desc.w + 2 * desc.pad_w - desc.s) // desc.stride_w + 1
         if dy.numel() != desc.n * desc.k * p * q or dw.numel() != desc.k * desc.c * desc.r * desc.s or dy.dtype != self.dtype or dw.dtype != torch.float32:
             raise ValueError("dy %s %s or dw %s %s is not the layer's" % (tuple(dy.shape), dy.dtype, tuple(dw.shape), dw.dtype))
+        if not is_dense(dy) or not is_dense(dw):          # (the kernels go by desc's layouts alone: past the end of an expanded tensor, over what lies between the rows of a view)
+            raise ValueError("dy %s with strides %s or dw %s with strides %s has gaps or repeated elements" % (tuple(dy.shape), dy.stride(), tuple(dw.shape), dw.stride()))
         with torch.cuda.device(self.codes.device):
             workspace = B.attach_packed_workspace(desc, methods=(method,), device=self.codes.device)
             B.gaconv_dw_from_packed(method, self.codes, self.scales, self.format, dy, dw, desc, seed)

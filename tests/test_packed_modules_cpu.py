@@ -52,3 +52,21 @@ def test_tensors_on_several_devices_are_refused(calls):
         with pytest.raises(ValueError, match="several devices"):
             packed.filter_gradient(dy, dw, linear_desc())
     assert not calls
+
+
+def test_gradients_with_gaps_or_repeats_are_refused(calls):
+    """An expanded gradient ends before the kernel does; what lies between the rows of a view is not the gradient's."""
+    packed = PackedActivation(4, 16, torch.bfloat16, "e4m3", "cpu")
+    one, dw = torch.zeros(1, 8, dtype=torch.bfloat16), torch.zeros(8, 16)
+    for dy in (one.expand(4, 8), one[:, :1].expand(4, 8), torch.zeros(4, 10, dtype=one.dtype)[:, :8], torch.zeros(8, 8, dtype=one.dtype)[::2],
+               torch.zeros(64, dtype=one.dtype).as_strided((4, 8), (7, 1)), torch.zeros(64, dtype=one.dtype).as_strided((4, 8), (3, 3))):
+        with pytest.raises(ValueError, match="gaps"):
+            packed.filter_gradient(dy, dw, linear_desc())
+    for dw in (torch.zeros(8, 32)[:, :16], torch.zeros(1, 16).expand(8, 16)):
+        with pytest.raises(ValueError, match="gaps"):
+            packed.filter_gradient(torch.zeros(4, 8, dtype=one.dtype), dw, linear_desc())
+    assert not calls
+    for dy, dw in ((torch.zeros(4, 8, dtype=one.dtype), torch.zeros(8, 16)), (torch.zeros(8, 4, dtype=one.dtype).t(), torch.zeros(8, 16, 1, 1)),
+                   (torch.zeros(4, 8, 1, 1, dtype=one.dtype).contiguous(memory_format=torch.channels_last), torch.zeros(8, 16))):
+        packed.filter_gradient(dy, dw, linear_desc())
+        assert calls.pop()[0] == "gaconv_dw_from_packed"
