@@ -201,7 +201,7 @@ class _RMSNorm(torch.autograd.Function):
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         s = None if res is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
         rstd = torch.empty(n, dtype=torch.float32, device=x.device)
-        w = weight if weight.data_ptr() % 16 == 0 else weight.clone()
+        w = weight if weight.is_contiguous() and weight.data_ptr() % 16 == 0 else weight.clone(memory_format=torch.contiguous_format)
         with torch.cuda.device(x.device):
             d = B.make_rows_desc(n, cols, x.dtype, fmt=packed.format if packed else B.ACT_E4M3, eps=eps, x_stride=row_stride(rows),
                                  r_stride=0 if res is None else row_stride(res))

@@ -70,3 +70,14 @@ def test_gradients_with_gaps_or_repeats_are_refused(calls):
                    (torch.zeros(4, 8, 1, 1, dtype=one.dtype).contiguous(memory_format=torch.channels_last), torch.zeros(8, 16))):
         packed.filter_gradient(dy, dw, linear_desc())
         assert calls.pop()[0] == "gaconv_dw_from_packed"
+
+
+def test_norm_weights_that_are_not_dense(calls):
+    """A weight that is every other element of a longer one, or one element for all channels, is read as its values, not as the memory behind its first."""
+    x = torch.zeros(4, 16, dtype=torch.bfloat16)
+    norm = GARMSNorm(16, device="cpu")
+    for weight in (torch.arange(32.0).bfloat16()[::2], torch.ones(1).bfloat16().expand(16), torch.arange(40.0).bfloat16()[3:19]):
+        norm.weight = torch.nn.Parameter(weight)
+        norm(x)
+        given = calls.pop()[1][2]
+        assert given.is_contiguous() and given.data_ptr() % 16 == 0 and torch.equal(given, weight)
