@@ -236,6 +236,8 @@ def make_rows_desc(rows: int, cols: int, dtype: torch.dtype, *, fmt=ACT_E4M3, ep
     d = RowsDesc()
     d.struct_size = ctypes.sizeof(RowsDesc)
     d.rows, d.cols, d.format, d.eps = rows, cols, fmt, eps
+    if (d.rows, d.cols) != (rows, cols):          # (ctypes keeps the low bits of a number that a field has no room for)
+        raise GaconvError(ERR_UNSUPPORTED, "%d rows of %d channels" % (rows, cols))
     if dtype not in (torch.bfloat16, torch.float32):
         raise TypeError("rows are bf16 or fp32, not %s" % dtype)
     d.dtype = BF16 if dtype == torch.bfloat16 else F32

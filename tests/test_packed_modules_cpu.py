@@ -81,3 +81,11 @@ def test_norm_weights_that_are_not_dense(calls):
         norm(x)
         given = calls.pop()[1][2]
         assert given.is_contiguous() and given.data_ptr() % 16 == 0 and torch.equal(given, weight)
+
+
+@pytest.mark.parametrize("rows, cols", [(1, (1 << 32) + 8), (1, 1 << 31), ((1 << 64) + 4, 8), (1, 8 - (1 << 32))])
+def test_rows_that_the_descriptor_has_no_room_for(rows, cols):
+    """They were another, smaller problem: 8 channels of 2^32 + 8."""
+    with pytest.raises(B.GaconvError) as e:
+        B.make_rows_desc(rows, cols, torch.bfloat16)
+    assert e.value.status == B.ERR_UNSUPPORTED
