@@ -127,10 +127,14 @@ def _check(status: int, where: str):
 
 
 def _ptr(t):
+    if t is None:
+        return None
     try:
         return t.data_ptr()
-    except AttributeError:          # None, or an address
-        return t
+    except AttributeError:          # an address; ctypes would take the bytes of a bytes object for memory of a GPU, too
+        if isinstance(t, int):
+            return t
+        raise
 
 
 # the handle alone: torch.cuda.current_stream() builds a Stream object around it, 3 us a call where this takes 0.2
