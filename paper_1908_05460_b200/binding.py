@@ -143,6 +143,14 @@ _device = getattr(torch._C, "_cuda_getDevice", None)        # torch.cuda.current
 _cuda_runs = False
 
 
+def _after_fork():
+    global _cuda_runs
+    _cuda_runs = False          # a child cannot use its parent's CUDA: torch.cuda.current_device() says so
+
+
+os.register_at_fork(after_in_child=_after_fork)
+
+
 def _stream(stream):
     global _cuda_runs
     if stream is None:

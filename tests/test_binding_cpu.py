@@ -1,4 +1,6 @@
 """What the binding makes of its arguments and of the process around it: no GPU needed."""
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -22,3 +24,27 @@ def test_pointers_are_tensors_addresses_or_none():
             B._ptr(wrong)
         with pytest.raises(AttributeError):
             B.gaconv_act_pack(wrong, t, t, desc, 0)
+
+
+def test_a_forked_process_hears_it_from_torch(monkeypatch):
+    """A process forked after CUDA has started cannot use it, and torch.cuda.current_device() says so; the short way to the stream does not ask."""
+    ways = []
+    monkeypatch.setattr(B, "_cuda_runs", True)
+    monkeypatch.setattr(B, "_device", lambda: 0)
+    monkeypatch.setattr(B, "_raw_stream", lambda device: ways.append("short") or 7)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: ways.append("torch") or 0)
+    assert B._stream(None) == 7 and ways == ["short"]
+    read, write = os.pipe()
+    pid = os.fork()
+    if pid == 0:
+        try:
+            del ways[:]
+            B._stream(None)
+            os.write(write, ways[0].encode())
+        finally:
+            os._exit(0)
+    os.close(write)
+    with os.fdopen(read, "rb") as f:
+        assert f.read() == b"torch"
+    os.waitpid(pid, 0)
+    assert B._cuda_runs          # the parent's own is left alone
