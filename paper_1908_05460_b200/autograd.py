@@ -134,9 +134,9 @@ class GAConv2d(torch.nn.Module):
 class _LinearFilterGrad(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, packed, fmt):
-        if ctx.needs_input_grad[1] and packed is None and x.numel() > 0:
-            packed = PackedActivation.pack(x, fmt)
-        kept, ctx.packed = packed.saved() if ctx.needs_input_grad[1] and packed is not None else ((), None)
+        kept, ctx.packed = (), None
+        if ctx.needs_input_grad[1] and x.numel() > 0 and weight.numel() > 0:
+            kept, ctx.packed = (PackedActivation.pack(x, fmt) if packed is None else packed).saved()
         ctx.save_for_backward(weight, *kept)
         return F.linear(x, weight, bias)
 
@@ -148,9 +148,9 @@ class _LinearFilterGrad(torch.autograd.Function):
         if ctx.needs_input_grad[0]:
             dx = dy.matmul(weight)
         if ctx.needs_input_grad[2]:
-            db = dy.reshape(-1, dy.shape[-1]).sum(0)
+            db = dy.flatten(0, -2).sum(0) if dy.dim() > 1 else dy.clone()
         if ctx.needs_input_grad[1]:
-            dw = torch.zeros_like(weight) if dy.numel() == 0 else linear_filter_gradient(PackedActivation.restored(kept, ctx.packed), dy).to(weight.dtype)
+            dw = torch.zeros_like(weight) if ctx.packed is None else linear_filter_gradient(PackedActivation.restored(kept, ctx.packed), dy).to(weight.dtype)
         return dx, dw, db, None, None
 
 

@@ -89,3 +89,16 @@ def test_rows_that_the_descriptor_has_no_room_for(rows, cols):
     with pytest.raises(B.GaconvError) as e:
         B.make_rows_desc(rows, cols, torch.bfloat16)
     assert e.value.status == B.ERR_UNSUPPORTED
+
+
+@pytest.mark.filterwarnings("ignore:Initializing zero-element")
+@pytest.mark.parametrize("shape, features", [((3, 0), 5), ((2, 3, 0), 5), ((0,), 5), ((3, 5), 0), ((2, 3, 5), 0), ((5,), 0), ((0, 5), 4), ((2, 0, 5), 4), ((3, 0), 0)])
+def test_linear_layers_without_tokens_or_features(shape, features, calls):
+    """Nothing is kept, and the gradients are torch's."""
+    layer, plain = GALinear(shape[-1], features, dtype=torch.float32, device="cpu"), torch.nn.Linear(shape[-1], features)
+    x, z = torch.zeros(shape, requires_grad=True), torch.zeros(shape, requires_grad=True)
+    layer(x).sum().backward()
+    plain(z).sum().backward()
+    for got, want in ((x.grad, z.grad), (layer.weight.grad, plain.weight.grad), (layer.bias.grad, plain.bias.grad)):
+        assert got.shape == want.shape and torch.equal(got, want)
+    assert not calls
