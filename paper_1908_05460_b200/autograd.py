@@ -24,6 +24,11 @@ from .layers import ConvLayer
 from .packed import DTYPES, PackedActivation, as_rows, check_devices, check_format, row_stride
 
 
+def _on_boundary(t, memory_format):
+    """t, of that format, where it starts on 16 bytes, or a copy that does."""
+    return t if t.data_ptr() % 16 == 0 else t.clone(memory_format=memory_format)
+
+
 class _Conv2dFilterGrad(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, module):
@@ -95,10 +100,11 @@ class GAConv2d(torch.nn.Module):
 
     @staticmethod
     def _dy_in_place(dy):
-        """dy as the library takes it, and its layout: the gradient of a channels-last forward arrives channels-last and is taken as it is ([N,P,Q,K] memory)"""
+        """dy as the library takes it, and its layout: the gradient of a channels-last forward arrives channels-last and is taken as it is ([N,P,Q,K] memory).
+        A part of a larger gradient (torch.cat's, of a batch) may start anywhere, and is copied unless that is a 16-byte boundary."""
         if dy.dim() == 4 and dy.shape[1] > 1 and not dy.is_contiguous() and dy.is_contiguous(memory_format=torch.channels_last):
-            return dy, B.DY_NPQK
-        return dy.contiguous(), B.DY_NKPQ                           # [N,K,P,Q]
+            return _on_boundary(dy, torch.channels_last), B.DY_NPQK
+        return _on_boundary(dy.contiguous(), torch.contiguous_format), B.DY_NKPQ                           # [N,K,P,Q]
 
     def packed_filter_gradient(self, packed, shape, dy):
         """filter_gradient for activations of `shape` that were kept in 8 bits."""
@@ -118,7 +124,7 @@ class GAConv2d(torch.nn.Module):
     def filter_gradient(self, x, dy):
         """dW [K,C,R,S] (the weight's dtype) of this layer for activations x and output gradient dy."""
         B.load()
-        x = x.contiguous(memory_format=torch.channels_last)        # NHWC memory under an NCHW-shaped tensor
+        x = _on_boundary(x.contiguous(memory_format=torch.channels_last), torch.channels_last)        # NHWC memory under an NCHW-shaped tensor
         if dy.dtype != x.dtype:
             dy = dy.to(x.dtype)
         dy, dy_layout = self._dy_in_place(dy)

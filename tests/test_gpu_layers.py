@@ -1,0 +1,33 @@
+"""The layers as parts of larger programs on the GPU: gradients that arrive as parts of others, evaluation, status of calls whose scratch is gone."""
+import numpy as np
+import pytest
+import torch
+
+import act8_ref as R
+from oracle import oracle
+from paper_1908_05460_b200.autograd import GAConv2d
+from paper_1908_05460_b200.packed import FORMATS
+
+pytestmark = pytest.mark.gpu
+TOL = 129 * 2.0 ** -23          # of the sum of magnitudes: chains of at most 128 additions, each off by 2^-23 of the running sum, and the planes of fp32 operands
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("order", [torch.contiguous_format, torch.channels_last])
+@pytest.mark.parametrize("checkpoint", [None, "e4m3"])
+def test_outputs_joined_by_cat(checkpoint, order, dtype):
+    """The second branch's gradient starts 3 * 13 * 49 elements into the joint one, off the 16-byte boundary."""
+    torch.manual_seed(11)
+    layers = [GAConv2d(5, 13, 3, 1, 1, dtype=dtype, checkpoint=checkpoint) for _ in range(2)]
+    x = torch.randn(6, 5, 7, 7, device="cuda").to(dtype).contiguous(memory_format=torch.channels_last)
+    parts = [x[:3], x[3:]]
+    dy = (0.01 * torch.randn(6, 13, 7, 7, device="cuda")).to(dtype).contiguous(memory_format=order)
+    assert dy[3:].data_ptr() % 16 != 0
+    torch.cat([layer(part) for layer, part in zip(layers, parts)]).backward(dy)
+    for layer, part, grad in zip(layers, parts, (dy[:3], dy[3:])):
+        x64 = R.f64(part)
+        if checkpoint is not None:
+            x64 = R.pack(R.f64(part.permute(0, 2, 3, 1).reshape(-1, 5)), FORMATS[checkpoint])[2].reshape(3, 7, 7, 5).transpose(0, 3, 1, 2)
+        want, size = oracle.dw_exact(x64, R.f64(grad), oracle.Shape(3, 5, 7, 7, 13, 3, 3, 1, 1, 1, 1))
+        assert np.all(np.abs(R.f64(layer.weight.grad) - want) <= HALF[dtype] * np.abs(want) + TOL * size)

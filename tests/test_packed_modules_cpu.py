@@ -6,7 +6,7 @@ import torch
 
 from paper_1908_05460_b200 import binding as B
 from paper_1908_05460_b200 import build as build_mod
-from paper_1908_05460_b200.autograd import GALinear, GARMSNorm
+from paper_1908_05460_b200.autograd import GAConv2d, GALinear, GARMSNorm
 from paper_1908_05460_b200.layers import ConvLayer
 from paper_1908_05460_b200.packed import PackedActivation
 
@@ -102,3 +102,25 @@ def test_linear_layers_without_tokens_or_features(shape, features, calls):
     for got, want in ((x.grad, z.grad), (layer.weight.grad, plain.weight.grad), (layer.bias.grad, plain.bias.grad)):
         assert got.shape == want.shape and torch.equal(got, want)
     assert not calls
+
+
+@pytest.mark.parametrize("checkpoint", [None, "e4m3"])
+@pytest.mark.parametrize("order", [torch.contiguous_format, torch.channels_last])
+def test_convolution_gradients_off_the_boundary(checkpoint, order, calls):
+    """The gradients of two outputs that torch.cat has joined are parts of one tensor, the second one's from an odd element on; an input may be such a part, too."""
+    layer = GAConv2d(4, 13, 3, 1, 1, dtype=torch.bfloat16, device="cpu", checkpoint=checkpoint)
+    whole = torch.zeros(6 * 13 * 49, dtype=torch.bfloat16)
+    dy = (whole.view(6, 13, 7, 7) if order is torch.contiguous_format else whole.view(6, 7, 7, 13).permute(0, 3, 1, 2))[3:]
+    dy.copy_(torch.randn(dy.shape))
+    x = torch.zeros(6 * 4 * 49 + 5, dtype=torch.bfloat16)[5:].view(6, 7, 7, 4).permute(0, 3, 1, 2)[3:]
+    assert dy.data_ptr() % 16 != 0 and x.data_ptr() % 16 != 0 and dy.is_contiguous(memory_format=order)
+    if checkpoint is None:
+        layer.filter_gradient(x, dy)
+        (_, _), (name, (given_x, given, _, desc)) = calls
+        assert name == "gaconv_dw_exact" and given_x.data_ptr() % 16 == 0 and given_x.is_contiguous(memory_format=torch.channels_last)
+    else:
+        layer.packed_filter_gradient(PackedActivation(3 * 49, 4, x.dtype, checkpoint, "cpu"), x.shape, dy)
+        name, (_, _, _, _, given, _, desc, _) = calls[-1]
+        assert name == "gaconv_dw_from_packed"
+    assert given.data_ptr() % 16 == 0 and given.is_contiguous(memory_format=order) and torch.equal(given, dy)
+    assert desc.dy_layout == (B.DY_NPQK if order is torch.channels_last else B.DY_NKPQ)
