@@ -85,6 +85,9 @@ class GAConv2d(torch.nn.Module):
         self._desc_cache = {}
 
     def forward(self, x):
+        # (inside a Function needs_input_grad is true of a weight with requires_grad, whether or not gradients are recorded)
+        if not torch.is_grad_enabled():
+            return F.conv2d(x.contiguous(memory_format=torch.channels_last), self.weight, None, self.stride, self.padding)
         return _Conv2dFilterGrad.apply(x.contiguous(memory_format=torch.channels_last), self.weight, self)
 
     def _desc(self, x, dy_layout=B.DY_NKPQ):
@@ -189,13 +192,15 @@ class GALinear(torch.nn.Module):
         check_devices(input=x, weight=self.weight, kept=None if packed is None else packed.codes)
         if packed is not None and (packed.rows * packed.cols != x.numel() or packed.cols != x.shape[-1] or packed.dtype != x.dtype):
             raise ValueError("the kept input has %d x %d values of %s, the input %s" % (packed.rows, packed.cols, packed.dtype, tuple(x.shape)))
+        if not torch.is_grad_enabled():          # (as in GAConv2d)
+            return F.linear(x, self.weight, self.bias)
         return _LinearFilterGrad.apply(x, self.weight, self.bias, packed, self.checkpoint)
 
 
 class NormOutput(NamedTuple):
     y: torch.Tensor
     sum: Optional[torch.Tensor]                 # x + residual, the next residual; None without one
-    packed: Optional[PackedActivation]          # y in 8 bits; None without `checkpoint`
+    packed: Optional[PackedActivation]          # y in 8 bits; None without `checkpoint` or `keep`
 
 
 class _RMSNorm(torch.autograd.Function):
@@ -239,7 +244,7 @@ class _RMSNorm(torch.autograd.Function):
 
 class GARMSNorm(torch.nn.Module):
     """Root-mean-square norm of the last dimension, of x + residual where one is given; with `checkpoint` its output comes in 8 bits as well, for the linear layers
-    behind it.  Returns NormOutput(y, sum, packed)."""
+    behind it.  Returns NormOutput(y, sum, packed).  `keep=False` in a call: without the 8-bit form, for evaluation, where no layer reads it."""
 
     def __init__(self, features, eps=1e-6, checkpoint=None, dtype=torch.bfloat16, device="cuda"):
         super().__init__()
@@ -248,12 +253,12 @@ class GARMSNorm(torch.nn.Module):
         self.eps, self.checkpoint = eps, check_format(checkpoint)
         self.weight = torch.nn.Parameter(torch.ones(features, dtype=dtype, device=device))
 
-    def forward(self, x, residual=None) -> NormOutput:
+    def forward(self, x, residual=None, keep=True) -> NormOutput:
         if x.dtype != self.weight.dtype or x.shape[-1] != self.weight.shape[0] or (residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype)):
             raise ValueError("input %s %s for a norm of %s %s, and a residual alike" % (tuple(x.shape), x.dtype, tuple(self.weight.shape), self.weight.dtype))
         check_devices(input=x, residual=residual, weight=self.weight)
         packed = None
-        if self.checkpoint is not None:
+        if self.checkpoint is not None and keep:
             packed = PackedActivation(x.numel() // x.shape[-1], x.shape[-1], x.dtype, self.checkpoint, x.device)
         out = _RMSNorm.apply(x, residual, self.weight, self.eps, packed)
         return NormOutput(out, None, packed) if residual is None else NormOutput(out[0], out[1], packed)

@@ -5,7 +5,8 @@ import torch
 
 import act8_ref as R
 from oracle import oracle
-from paper_1908_05460_b200.autograd import GAConv2d
+from paper_1908_05460_b200 import binding as B
+from paper_1908_05460_b200.autograd import GAConv2d, GALinear, GARMSNorm
 from paper_1908_05460_b200.packed import FORMATS
 
 pytestmark = pytest.mark.gpu
@@ -31,3 +32,18 @@ def test_outputs_joined_by_cat(checkpoint, order, dtype):
             x64 = R.pack(R.f64(part.permute(0, 2, 3, 1).reshape(-1, 5)), FORMATS[checkpoint])[2].reshape(3, 7, 7, 5).transpose(0, 3, 1, 2)
         want, size = oracle.dw_exact(x64, R.f64(grad), oracle.Shape(3, 5, 7, 7, 13, 3, 3, 1, 1, 1, 1))
         assert np.all(np.abs(R.f64(layer.weight.grad) - want) <= HALF[dtype] * np.abs(want) + TOL * size)
+
+
+def test_evaluation_launches_nothing():
+    """GALinear and GAConv2d without gradients: torch's forward and no kernel of this library; the norm alone, without codes."""
+    torch.manual_seed(12)
+    linear, conv, norm = GALinear(72, 40), GAConv2d(8, 16, 3, 1, 1, checkpoint="e4m3"), GARMSNorm(72, checkpoint="int8")
+    x, maps = torch.randn(9, 72, device="cuda").bfloat16(), torch.randn(2, 8, 6, 6, device="cuda")
+    y, z, n = linear(x), conv(maps), norm(x).y
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            before = B.gaconv_launch_count()
+            assert torch.equal(linear(x), y) and torch.equal(conv(maps), z)
+            assert B.gaconv_launch_count() == before
+            out = norm(x, keep=False)
+            assert out.packed is None and torch.equal(out.y, n) and B.gaconv_launch_count() == before + 1

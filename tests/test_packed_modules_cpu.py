@@ -124,3 +124,24 @@ def test_convolution_gradients_off_the_boundary(checkpoint, order, calls):
         assert name == "gaconv_dw_from_packed"
     assert given.data_ptr() % 16 == 0 and given.is_contiguous(memory_format=order) and torch.equal(given, dy)
     assert desc.dy_layout == (B.DY_NPQK if order is torch.channels_last else B.DY_NKPQ)
+
+
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.inference_mode])
+def test_evaluation_keeps_nothing(mode, calls):
+    """Where no gradients are recorded nothing is packed, though the weights require them; the norm's 8-bit form can be left out."""
+    linear, conv = GALinear(16, 8, device="cpu"), GAConv2d(4, 8, 3, 1, 1, device="cpu", checkpoint="int8")
+    norm = GARMSNorm(16, device="cpu", checkpoint="int8")
+    x, maps = torch.randn(3, 16).bfloat16(), torch.randn(2, 4, 5, 5)
+    with mode():
+        y, z = linear(x), conv(maps)
+        assert not calls
+        assert torch.equal(y, torch.nn.functional.linear(x, linear.weight, linear.bias)) and torch.equal(z, torch.nn.functional.conv2d(maps, conv.weight, None, 1, 1))
+        assert linear(x, PackedActivation(3, 16, x.dtype, "e4m3", "cpu")).shape == (3, 8)
+        out = norm(x, keep=False)
+        assert out.packed is None and out.y.shape == x.shape
+        name, given = calls.pop()
+        assert name == "gaconv_rmsnorm_forward" and given[5] is None and given[6] is None
+        assert norm(x).packed is not None
+    calls.clear()
+    linear(x), conv(maps)
+    assert [name for name, _ in calls] == ["gaconv_act_pack"] * 2
