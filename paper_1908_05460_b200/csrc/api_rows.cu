@@ -22,7 +22,7 @@ gaconv_status_t check_rows(const gaconv_rows_desc_t* d, gaconv_rows_desc_t* out)
     for (int64_t* s : {&out->x_stride, &out->r_stride, &out->s_stride, &out->y_stride}) {
         if (*s == 0) *s = d->cols;
         if (*s < d->cols) return GACONV_ERR_BAD_DESC;
-        if (*s > (1ll << 40)) return GACONV_ERR_UNSUPPORTED;       // (offsets stay far below 2^63 elements)
+        if (*s > (1ll << 40) || (d->rows > 0 && *s > (1ll << 60) / d->rows)) return GACONV_ERR_UNSUPPORTED;       // (offsets stay below 2^63 bytes)
     }
     return d->rows > 0x7fffffffll || d->cols > (1 << 28) ? GACONV_ERR_UNSUPPORTED : GACONV_OK;
 }

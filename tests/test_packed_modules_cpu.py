@@ -145,3 +145,16 @@ def test_evaluation_keeps_nothing(mode, calls):
     calls.clear()
     linear(x), conv(maps)
     assert [name for name, _ in calls] == ["gaconv_act_pack"] * 2
+
+
+def test_offsets_beyond_64_bits_are_refused():
+    """Rows times their distance, in bytes, is a number of the kernels' address arithmetic."""
+    for stride, rows, fine in ((1 << 40, 1 << 20, True), (1 << 40, (1 << 20) + 1, False), (1 << 40, (1 << 31) - 1, False), (1 << 29, (1 << 31) - 1, True), ((1 << 29) + 2, (1 << 31) - 1, False)):
+        for name in ("x_stride", "r_stride", "s_stride", "y_stride"):
+            desc = B.make_rows_desc(rows, 8, torch.float32, **{name: stride})
+            if fine:
+                assert B.gaconv_act_sizes(desc) == (rows * 16, rows)
+            else:
+                with pytest.raises(B.GaconvError) as e:
+                    B.gaconv_act_sizes(desc)
+                assert e.value.status == B.ERR_UNSUPPORTED
