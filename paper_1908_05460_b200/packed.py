@@ -102,8 +102,11 @@ class PackedActivation:
             raise ValueError("dy %s %s or dw %s %s is not the layer's" % (tuple(dy.shape), dy.dtype, tuple(dw.shape), dw.dtype))
         if not is_dense(dy) or not is_dense(dw):          # (the kernels go by desc's layouts alone: past the end of an expanded tensor, over what lies between the rows of a view)
             raise ValueError("dy %s with strides %s or dw %s with strides %s has gaps or repeated elements" % (tuple(dy.shape), dy.stride(), tuple(dw.shape), dw.stride()))
+        own = desc.workspace, desc.workspace_bytes
         with torch.cuda.device(self.codes.device):
-            workspace = B.attach_packed_workspace(desc, methods=(method,), device=self.codes.device)
-            B.gaconv_dw_from_packed(method, self.codes, self.scales, self.format, dy, dw, desc, seed)
-            desc.workspace, desc.workspace_bytes = None, 0
+            try:
+                workspace = B.attach_packed_workspace(desc, methods=(method,), device=self.codes.device)
+                B.gaconv_dw_from_packed(method, self.codes, self.scales, self.format, dy, dw, desc, seed)
+            finally:          # (a descriptor that went on pointing at this call's workspace would have later calls write to memory that is others' by then)
+                desc.workspace, desc.workspace_bytes = own
         del workspace          # (back to the allocator, which hands it out again in the order of this stream)

@@ -158,3 +158,21 @@ def test_offsets_beyond_64_bits_are_refused():
                 with pytest.raises(B.GaconvError) as e:
                     B.gaconv_act_sizes(desc)
                 assert e.value.status == B.ERR_UNSUPPORTED
+
+
+def test_a_descriptor_keeps_its_own_workspace(calls, monkeypatch):
+    """filter_gradient brings a workspace for the call; afterwards the descriptor has the caller's again, or none, also where the library refuses."""
+    packed, dy, dw = PackedActivation(4, 16, torch.bfloat16, "e4m3", "cpu"), torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(8, 16)
+    seen = []
+    for refuse in (False, True):
+        def call(*a):
+            seen.append(a[6].workspace)
+            if refuse:
+                raise B.GaconvError(B.ERR_BAD_DESC, "gaconv_dw_from_packed")
+        monkeypatch.setattr(B, "gaconv_dw_from_packed", call)
+        for own in ((None, 0), (4096, 512)):
+            desc = linear_desc()
+            desc.workspace, desc.workspace_bytes = own
+            with pytest.raises(B.GaconvError) if refuse else contextlib.nullcontext():
+                packed.filter_gradient(dy, dw, desc)
+            assert (desc.workspace, desc.workspace_bytes) == own and seen.pop() not in (None, 4096)
