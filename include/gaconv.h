@@ -14,7 +14,7 @@
  *     are host memory (pinned for true asynchrony).  The library allocates no device memory and keeps
  *     no reference to any buffer after the call returns (the work itself is asynchronous, see below).
  *   - `stream` is a cudaStream_t passed as void*.  All work is enqueued on it; no entry point
- *     synchronises the host except gaconv_poll_async_status and gaconv_dw_from_host's final wait
+ *     synchronises the host except the gaconv_poll_* calls and gaconv_dw_from_host's final wait
  *     (gaconv_dw_from_host_async has none).
  *   - Validation errors are returned at once and enqueue nothing.
  *   - dw is overwritten (no accumulate-into).  It is always fp32.
@@ -260,6 +260,12 @@ gaconv_status_t gaconv_rmsnorm_workspace_size(const gaconv_rows_desc_t *desc, si
 /* Waits for `stream`, then reports GACONV_ERR_TIMEOUT if a kernel that used desc->workspace gave up
  * on a bounded wait since the last poll (and clears the flag), GACONV_OK otherwise. */
 gaconv_status_t gaconv_poll_async_status(const gaconv_conv_desc_t *desc, void *stream);
+/* For workspaces that are given back before they are polled: enqueues, behind the calls that used desc->workspace on `stream`, a kernel that adds its
+ * status to one of the current device's own (a variable of the library), and the workspace is free once that has run. */
+gaconv_status_t gaconv_collect_async_status(const gaconv_conv_desc_t *desc, void *stream);
+/* Waits for `stream`, then reports GACONV_ERR_TIMEOUT if a status that was collected on the current device since the last such
+ * report was raised (and clears it), GACONV_OK otherwise. */
+gaconv_status_t gaconv_poll_collected_status(void *stream);
 
 /* ---- approximation schedules (Section 2.5): which method each layer uses at each training batch ---- */
 typedef struct gaconv_schedule gaconv_schedule_t;   /* host object, owned by the caller via create/destroy */

@@ -197,6 +197,24 @@ class GALinear(torch.nn.Module):
         return _LinearFilterGrad.apply(x, self.weight, self.bias, packed, self.checkpoint)
 
 
+def check_async_status(*modules: torch.nn.Module):
+    """Raises GaconvError if a kernel of a filter gradient gave up on a bounded wait since the last look, so that the gradient is not to be used.
+
+    Waits for the current stream of each device, so it belongs where a program reads its loss.  Looked at are the gradients from inputs that were kept in 8 bits, of
+    whatever layer, on the devices that `modules` have parameters on (none given: the current one), and those of the GAConv2d layers in `modules`."""
+    failed = []
+    devices = {p.device for module in modules for p in module.parameters() if p.is_cuda}
+    for device in sorted(devices, key=str) if modules else [None]:
+        with torch.cuda.device(device):
+            failed.append(B.gaconv_poll_collected_status())
+    for layer in (m for module in modules for m in module.modules() if isinstance(m, GAConv2d)):
+        for desc, workspace in layer._desc_cache.values():
+            with torch.cuda.device(workspace.device):
+                failed.append(B.gaconv_poll_async_status(desc))
+    for status in failed:          # (every word has been looked at and cleared)
+        B._check(status, "check_async_status")
+
+
 class NormOutput(NamedTuple):
     y: torch.Tensor
     sum: Optional[torch.Tensor]                 # x + residual, the next residual; None without one

@@ -37,6 +37,7 @@ EXPORTS = [
     "gaconv_schedule_create", "gaconv_schedule_method", "gaconv_schedule_run_layer", "gaconv_schedule_run_step", "gaconv_schedule_destroy",
     "gaconv_act_sizes", "gaconv_act_pack", "gaconv_act_unpack", "gaconv_dw_from_packed", "gaconv_packed_workspace_size",
     "gaconv_rmsnorm_forward", "gaconv_rmsnorm_backward", "gaconv_rmsnorm_workspace_size",
+    "gaconv_collect_async_status", "gaconv_poll_collected_status",
     "gaconv_dw_exact_static", "gaconv_static_scratch_bytes", "gaconv_poll_async_status_static", "gaconv_approx_select_topk",
 ]
 
@@ -91,6 +92,8 @@ def load():
     lib.gaconv_dw_from_host_async.argtypes = [i32, vp, vp, vp, vp, vp, vp, dp, u64, vp]
     lib.gaconv_poll_async_status.argtypes = [dp, vp]
     lib.gaconv_poll_async_status_static.argtypes = [vp]
+    lib.gaconv_collect_async_status.argtypes = [dp, vp]
+    lib.gaconv_poll_collected_status.argtypes = [vp]
     lib.gaconv_approx_select_topk.argtypes = [vp, vp, vp, dp, vp]
     rp = ctypes.POINTER(RowsDesc)
     lib.gaconv_act_sizes.argtypes = [rp, ctypes.POINTER(sz), ctypes.POINTER(sz)]
@@ -311,6 +314,14 @@ def gaconv_rmsnorm_backward(dy, dsum, sum_, weight, rstd, dx, dweight, desc: Row
     _check((_lib or load()).gaconv_rmsnorm_backward(_ptr(dy), _ptr(dsum), _ptr(sum_), _ptr(weight), _ptr(rstd), _ptr(dx), _ptr(dweight),
                                           ctypes.byref(desc), _ptr(workspace), 0 if workspace is None else workspace.numel(),
                                           _stream(stream)), "gaconv_rmsnorm_backward")
+
+
+def gaconv_collect_async_status(desc: ConvDesc, stream=None):
+    _check((_lib or load()).gaconv_collect_async_status(ctypes.byref(desc), _stream(stream)), "gaconv_collect_async_status")
+
+
+def gaconv_poll_collected_status(stream=None) -> int:
+    return load().gaconv_poll_collected_status(_stream(stream))
 
 
 def gaconv_poll_async_status(desc: ConvDesc, stream=None) -> int:

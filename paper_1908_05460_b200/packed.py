@@ -107,6 +107,7 @@ class PackedActivation:
             try:
                 workspace = B.attach_packed_workspace(desc, methods=(method,), device=self.codes.device)
                 B.gaconv_dw_from_packed(method, self.codes, self.scales, self.format, dy, dw, desc, seed)
+                B.gaconv_collect_async_status(desc)          # (whether a kernel gave up is asked when the workspace is gone: autograd.check_async_status)
             finally:          # (a descriptor that went on pointing at this call's workspace would have later calls write to memory that is others' by then)
                 desc.workspace, desc.workspace_bytes = own
         del workspace          # (back to the allocator, which hands it out again in the order of this stream)

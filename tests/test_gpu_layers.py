@@ -6,7 +6,8 @@ import torch
 import act8_ref as R
 from oracle import oracle
 from paper_1908_05460_b200 import binding as B
-from paper_1908_05460_b200.autograd import GAConv2d, GALinear, GARMSNorm
+from paper_1908_05460_b200.autograd import GAConv2d, GALinear, GARMSNorm, check_async_status
+from paper_1908_05460_b200.graph_names import kernel_names
 from paper_1908_05460_b200.packed import FORMATS
 
 pytestmark = pytest.mark.gpu
@@ -47,3 +48,53 @@ def test_evaluation_launches_nothing():
             assert B.gaconv_launch_count() == before
             out = norm(x, keep=False)
             assert out.packed is None and torch.equal(out.y, n) and B.gaconv_launch_count() == before + 1
+
+
+def test_status_outlives_the_workspace(monkeypatch):
+    """A status word that is raised in a call's workspace (from the host: no wait is made to run out) is reported after the workspace went back and was used again, once."""
+    torch.manual_seed(13)
+    layer, conv = GALinear(72, 40), GAConv2d(8, 16, 3, 1, 1, checkpoint="e4m3")
+    x, maps = torch.randn(9, 72, device="cuda").bfloat16(), torch.randn(2, 8, 6, 6, device="cuda")
+    check_async_status(layer, conv)
+    attach, run = B.attach_packed_workspace, B.gaconv_dw_from_packed
+    held = []
+
+    def attach_and_hold(*a, **k):
+        held.append(attach(*a, **k))
+        return held[-1]
+
+    def run_and_give_up(*a):
+        run(*a)
+        held.pop()[:4].copy_(torch.tensor([1, 0, 0, 0], dtype=torch.uint8))
+    for module, inp in ((layer, x), (conv, maps)):
+        with monkeypatch.context() as m:
+            m.setattr(B, "attach_packed_workspace", attach_and_hold)
+            m.setattr(B, "gaconv_dw_from_packed", run_and_give_up)
+            module(inp).sum().backward()
+        for _ in range(3):          # later calls, in the same memory
+            module(inp).sum().backward()
+        with pytest.raises(B.GaconvError) as e:
+            check_async_status(module)
+        assert e.value.status == B.ERR_TIMEOUT
+        check_async_status(module)
+        check_async_status()
+
+
+def test_status_of_a_captured_step():
+    """The collection is part of a captured backward pass; a word that the graph's call does not raise stays down."""
+    torch.manual_seed(14)
+    layer = GALinear(64, 48)
+    x = torch.randn(40, 64, device="cuda").bfloat16()
+    step = lambda: torch.autograd.grad(layer(x).float().square().sum(), [layer.weight])[0]  # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        want = step().clone()
+    torch.cuda.current_stream().wait_stream(side)
+    assert sum("collect_status" in name for name in kernel_names(step)) == 1
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    graph.replay()
+    check_async_status(layer)
+    assert torch.equal(got, want)

@@ -1,12 +1,13 @@
 """What the layers that keep their inputs in 8 bits hand to the library, and what they refuse: no GPU needed, the library's calls are replaced by recorders."""
 import contextlib
+import ctypes
 
 import pytest
 import torch
 
 from paper_1908_05460_b200 import binding as B
 from paper_1908_05460_b200 import build as build_mod
-from paper_1908_05460_b200.autograd import GAConv2d, GALinear, GARMSNorm
+from paper_1908_05460_b200.autograd import GAConv2d, GALinear, GARMSNorm, check_async_status
 from paper_1908_05460_b200.layers import ConvLayer
 from paper_1908_05460_b200.packed import PackedActivation
 
@@ -25,6 +26,7 @@ def calls(monkeypatch):
     made = []
     for name in ENQUEUE:
         monkeypatch.setattr(B, name, lambda *a, name=name, **k: made.append((name, a)))
+    monkeypatch.setattr(B, "gaconv_collect_async_status", lambda *a, **k: None, raising=False)
     monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
     return made
 
@@ -176,3 +178,56 @@ def test_a_descriptor_keeps_its_own_workspace(calls, monkeypatch):
             with pytest.raises(B.GaconvError) if refuse else contextlib.nullcontext():
                 packed.filter_gradient(dy, dw, desc)
             assert (desc.workspace, desc.workspace_bytes) == own and seen.pop() not in (None, 4096)
+
+
+def test_a_kernel_that_gave_up_is_reported(calls, monkeypatch):
+    """The workspace of a layer's call is given back at once; its status is collected before, and check_async_status raises for it once."""
+    raised = [B.OK]
+    workspaces = []
+    monkeypatch.setattr(B, "gaconv_workspace_init", lambda ws, n, **k: workspaces.append(ws) or ws[:256].zero_())
+
+    def kernel(*a):
+        calls.append(("gaconv_dw_from_packed", a))
+        workspaces[-1][0] = 1          # what a kernel does that gives up
+
+    def collect(desc, stream=None):
+        ws = workspaces.pop()
+        assert desc.workspace == ws.data_ptr() and calls[-1][0] == "gaconv_dw_from_packed"
+        if int(ws[:4].view(torch.int32)) != 0:
+            raised[0] = B.ERR_TIMEOUT
+
+    def poll(stream=None):
+        status, raised[0] = raised[0], B.OK
+        return status
+    monkeypatch.setattr(B, "gaconv_dw_from_packed", kernel)
+    monkeypatch.setattr(B, "gaconv_collect_async_status", collect)
+    monkeypatch.setattr(B, "gaconv_poll_collected_status", poll)
+    layer = GALinear(16, 8, device="cpu")
+    check_async_status()
+    layer(torch.randn(3, 16).bfloat16()).sum().backward()
+    with pytest.raises(B.GaconvError) as e:
+        check_async_status()
+    assert e.value.status == B.ERR_TIMEOUT
+    check_async_status()
+    # a convolution without a checkpoint keeps its workspaces, which are asked one by one, all of them before anything is raised
+    conv = GAConv2d(4, 8, 3, 1, 1, device="cpu")
+    words = {}
+    for hw in (5, 6):
+        conv(torch.randn(2, 4, hw, hw)).sum().backward()
+    descs = [desc for desc, _ in conv._desc_cache.values()]
+    assert len(descs) == 2
+    words = {id(d): B.ERR_TIMEOUT for d in descs}
+    monkeypatch.setattr(B, "gaconv_poll_async_status", lambda desc, stream=None: words.pop(id(desc), B.OK))
+    with pytest.raises(B.GaconvError):
+        check_async_status(torch.nn.Sequential(conv))
+    check_async_status(conv)
+
+
+def test_status_calls_check_their_arguments():
+    lib, desc = B.load(), linear_desc()
+    ref = ctypes.byref(desc)
+    assert lib.gaconv_collect_async_status(None, None) == B.ERR_NULL_POINTER and lib.gaconv_collect_async_status(ref, None) == B.ERR_NULL_POINTER
+    desc.workspace, desc.workspace_bytes = 4096 + 8, 1 << 20
+    assert lib.gaconv_collect_async_status(ref, None) == B.ERR_MISALIGNED
+    desc.workspace, desc.workspace_bytes = 4096, 255
+    assert lib.gaconv_collect_async_status(ref, None) == B.ERR_WORKSPACE_TOO_SMALL
