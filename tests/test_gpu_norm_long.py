@@ -1,0 +1,39 @@
+"""The weight's gradient of the norm over very many rows.
+
+Terms of one sign, alike in every row, so that roundings do not cancel: a chain of n additions is then off by up to n u, u = 2^-24.  Bounds, in u of the sum: two roundings of a term; chains of
+64; how the chains are added up (64 u for the 63 chains of a team here, 2 u where what is rounded off is kept); 37 for the blocks' sums, five in a thread and 32 threads: 168 u and 106 u."""
+import numpy as np
+import pytest
+import torch
+
+import act8_ref as R
+from paper_1908_05460_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def weight_gradient(rows, cols, dtype, y_stride=0):
+    """dweight, and what it is in 64 bits, for rows that are all the same."""
+    g = torch.Generator().manual_seed(cols)
+    dy, s = ((0.5 + torch.rand(cols, generator=g)).to(dtype) for _ in range(2))
+    buf = torch.zeros(rows, y_stride or cols, dtype=dtype, device="cuda")
+    buf[:, :cols] = dy.cuda()
+    rstd = torch.full((rows,), 1.1, device="cuda")
+    dx, dw, w = torch.empty(rows, cols, dtype=dtype, device="cuda"), torch.empty(cols, device="cuda"), torch.ones(cols, dtype=dtype, device="cuda")
+    d = B.make_rows_desc(rows, cols, dtype, y_stride=y_stride)
+    B.gaconv_rmsnorm_backward(buf, None, s.cuda().repeat(rows, 1), w, rstd, dx, dw, d, B.rmsnorm_workspace(d))
+    return R.f64(dw), rows * R.f64(dy) * R.f64(s) * R.f64(rstd[:1])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_on_different_boundaries(dtype):
+    """dy's rows lie four elements apart, the sum's three: a thread a channel, 16384 rows each."""
+    got, want = weight_gradient(1 << 20, 3, dtype, 4)
+    assert np.all(np.abs(got - want) <= 106 * U * want)
+
+
+def test_rows_that_a_team_takes_in_turn():
+    """A row takes a block of 288 threads, and a block 4000 rows."""
+    got, want = weight_gradient(4000 * 148, 2052, torch.float32)
+    assert np.all(np.abs(got - want) <= 168 * U * want)
