@@ -273,7 +273,7 @@ rmsnorm_backward_kernel(const NormRows o, const T* dy, const T* ds, const T* s, 
             const int c = N * (i * lanes + l) - shift;
             pg[i].start(rg, c); ps[i].start(rh, c); pd[i].start(rd, c);
         }
-        if (live) rs_next = __ldg(rstd + row);
+        rs_next = live ? __ldg(rstd + row) : 0.f;          // (a row of nothing adds 0, not 0 times the last row's, which may be infinite)
     };
     start(first + team);
     for (; first < o.rows; first += step) {

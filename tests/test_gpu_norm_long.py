@@ -37,3 +37,19 @@ def test_rows_that_a_team_takes_in_turn():
     """A row takes a block of 288 threads, and a block 4000 rows."""
     got, want = weight_gradient(4000 * 148, 2052, torch.float32)
     assert np.all(np.abs(got - want) <= 168 * U * want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_an_infinite_rstd_stays_in_its_row(dtype):
+    """A row whose squares underflow has, without eps, an infinite rstd, and the weight's gradient is infinite; a team that then has no row left adds nothing to it."""
+    rows, cols = 148 * 64 + 1, 8          # (teams of 8 threads, 64 a block, a block an SM: one row is left for the second round)
+    s = torch.ones(rows, cols, dtype=dtype, device="cuda")
+    s[1:64] = 1e-25
+    w, y, rstd = torch.ones(cols, dtype=dtype, device="cuda"), torch.empty_like(s), torch.empty(rows, device="cuda")
+    d = B.make_rows_desc(rows, cols, dtype, eps=0.0)
+    B.gaconv_rmsnorm_forward(s, None, w, None, y, None, None, rstd, d)
+    assert torch.isinf(rstd[1:64]).all() and (rstd[64:] == 1).all()
+    dy, dx, dw = torch.ones_like(s), torch.empty_like(s), torch.empty(cols, device="cuda")
+    B.gaconv_rmsnorm_backward(dy, None, s, w, rstd, dx, dw, d, B.rmsnorm_workspace(d))
+    assert (dw == float("inf")).all()
+    assert torch.isfinite(dx[0]).all() and torch.isfinite(dx[64:]).all()
