@@ -1,6 +1,8 @@
 """What the layers that keep their inputs in 8 bits hand to the library, and what they refuse: no GPU needed, the library's calls are replaced by recorders."""
 import contextlib
 import ctypes
+import random
+from concurrent.futures import ThreadPoolExecutor
 
 import pytest
 import torch
@@ -231,3 +233,19 @@ def test_status_calls_check_their_arguments():
     assert lib.gaconv_collect_async_status(ref, None) == B.ERR_MISALIGNED
     desc.workspace, desc.workspace_bytes = 4096, 255
     assert lib.gaconv_collect_async_status(ref, None) == B.ERR_WORKSPACE_TOO_SMALL
+
+
+def test_plans_asked_for_by_several_threads():
+    """More sizes than the table of plans has room for, in other orders, by eight threads at once: each gets what one thread alone gets."""
+    sizes = [(m, c, k) for m in (1, 7, 100, 513, 4099, 20000) for c in (8, 33, 130, 512, 1000) for k in range(40, 1240, 80)]
+
+    def workspace(size):
+        return B.gaconv_packed_workspace_size(linear_desc(*size), B.METHOD_EXACT)
+    want = {size: workspace(size) for size in sizes}
+
+    def work(seed):
+        order = sizes * 3
+        random.Random(seed).shuffle(order)
+        return all(workspace(size) == want[size] for size in order)
+    with ThreadPoolExecutor(8) as pool:
+        assert all(pool.map(work, range(8)))
