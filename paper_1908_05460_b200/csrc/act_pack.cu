@@ -102,14 +102,14 @@ act_unpack_kernel(const uint8_t* codes, const uint8_t* scales, T* x, const RowsO
     }
 }
 
-// threads of a row: one a piece, but no more than an eighth of that many while there are rows enough
+// threads of a row: one a piece (at most a block), or, where there are rows enough, as few as a quarter of that: a thread then has the kAhead pieces whose loads it keeps in flight
 RowsOp rows_op(const ActRows& a)
 {
     RowsOp o;
     o.rows = a.rows; o.stride = a.stride; o.cols = a.cols; o.pitch = act_pitch(a.cols); o.groups = act_groups(a.cols);
     const int pieces = o.groups * (a.bf16 ? 4 : 8);
     o.log_lanes = 3;
-    while (o.log_lanes < 8 && (1 << o.log_lanes) < pieces && ((kAhead << o.log_lanes) < pieces || a.rows << o.log_lanes < 148 * 1024)) ++o.log_lanes;
+    while (o.log_lanes < 8 && (1 << o.log_lanes) < pieces && ((kAhead << o.log_lanes) < pieces || a.rows << o.log_lanes < device_sms() * 1024ll)) ++o.log_lanes;
     return o;
 }
 unsigned row_blocks(const RowsOp& o) { return (unsigned)((o.rows + (kBlock >> o.log_lanes) - 1) / (kBlock >> o.log_lanes)); }

@@ -1,10 +1,12 @@
 // Root-mean-square norm behind the addition of the residual, with its output in 8 bits as well, and its backward pass.
 //
-//   forward    s = x + r (rounded to the type),  rstd = 1 / sqrt(mean(s^2) + eps),  y = s rstd w (rounded once),  codes, scales = y in 8 bits (act8.cuh)
+//   forward    s = x + r (rounded to the type),  rstd = 1 / sqrt(mean(s^2) + eps),  y = s rstd w (fp32, then rounded to the type),  codes, scales = y in 8 bits (act8.cuh)
 //   backward   h = s rstd,  g = dy w,  dx = ds + rstd (g - h mean(g h)),  dw = sum over rows of dy h
 //
-// Bound by HBM: every tensor is read and written once.  A team of `lanes` threads holds a row in registers, `NU` pieces of 16 bytes a thread, by
-// columns where rows are whole pieces (FULL) and by their frame elsewhere (rows.cuh), so that the second use of a row (after its mean) reads nothing.  Sums and means are fp32, in an order that depends on the sizes alone.
+// Bound by HBM.  A team of `lanes` threads holds a row in registers, `NU` pieces of 16 bytes a thread, by columns where rows are whole pieces (FULL) and by
+// their frame elsewhere (rows.cuh), so that the second use of a row (after its mean) reads nothing: every tensor is read and written once.  Rows beyond the
+// registers, and tensors whose rows lie on different boundaries, take the kernels called long, which read what they need twice: forward its sum (or x), backward dy and the
+// sum, and both once more for the weight's gradient.  Sums and means are fp32, in an order that depends on the sizes alone.
 #include <algorithm>
 #include <type_traits>
 
@@ -68,9 +70,9 @@ __device__ __forceinline__ uint4 load_weight(const T* __restrict__ w, int c, int
 
 // Blocks stay and their teams take rows in turn, the next one's loads on their way while a row is worked on.  Where rows are not whole pieces a team's
 // rows are a multiple of N apart: they have one frame, and the weight's pieces in it stay in registers.
-// WIDE: registers for three blocks of 256 threads an SM.  Rows of more than 128 threads gain by it, shorter ones lose (us without, with: 16384x4096 bf16 104.6,
-// 100.8; 8192x3584 bf16 51.8, 49.8; 8000x1333 fp32 56.8, 48.6; 16384x1024 bf16 28.0, 29.3; 16000x333 fp32 36.6, 40.4; without codes 16384x4096 bf16 90.7, 94.0;
-// bf16 rows that are not whole pieces 8000x3003 66.9, 69.5; few of bf16 512x4096 6.2, 6.4).
+// WIDE: registers for three blocks of 256 threads an SM.  Rows of more than 128 threads gain by it, shorter ones lose (us of calls one behind the other, without
+// and with: 16384x4096 bf16 101.6, 99.2; 8192x3584 bf16 52.0, 50.8; 8000x1333 fp32 56.2, 48.7; 16384x1024 bf16 28.0, 29.3; 16000x333 fp32 36.6, 40.4; without codes
+// 16384x4096 bf16 90.7, 94.0; bf16 rows that are not whole pieces 8000x3003 66.9, 69.5; few of bf16 512x4096 6.2, 6.4).
 template <typename T, int NU, bool FULL, bool WIDE = false>
 __global__ void __launch_bounds__(WIDE ? 256 : 512, WIDE ? 3 : 1)
 rmsnorm_forward_kernel(const NormRows o, const T* x, const T* res, const T* __restrict__ w, T* sum, T* y, uint8_t* codes, uint8_t* scales, float* rstd, int lanes)
@@ -401,7 +403,7 @@ Team team_of(const NormRows& o, int most, long long a, long long b, long long c,
     const int pieces = t.full ? o.cols / n : (o.cols + 2 * n - 2) / n;         // (a frame starts up to n - 1 elements early)
     auto lanes = [&](int nu) { return (pieces + 32 * nu - 1) / (32 * nu) * 32; };
     if (!t.full && (a % n != b % n || a % n != c % n || a % n != d % n)) return t;
-    t.nu = lanes(1) == 32 || (lanes(1) <= kMaxTeam && o.rows * lanes(2) < 148 * 512) ? 1 : lanes(2) <= (most == 4 ? kMaxTeam / 2 : kMaxTeam) ? 2 : lanes(4) <= kMaxTeam && most == 4 ? 4 : 0;
+    t.nu = lanes(1) == 32 || (lanes(1) <= kMaxTeam && o.rows * lanes(2) < device_sms() * 512ll) ? 1 : lanes(2) <= (most == 4 ? kMaxTeam / 2 : kMaxTeam) ? 2 : lanes(4) <= kMaxTeam && most == 4 ? 4 : 0;
     if (t.nu != 0) t.lanes = pieces <= 8 ? 8 : pieces <= 16 ? 16 : lanes(t.nu);
     return t;
 }
