@@ -94,6 +94,8 @@ class PackedActivation:
     def filter_gradient(self, dy, dw, desc: B.ConvDesc, method: int = B.METHOD_EXACT, seed: int = 0):
         """gaconv_dw_from_packed in a workspace of this call's own; desc says what layer the rows belong to."""
         check_devices(kept=self.codes, dy=dy, dw=dw)
+        if desc.in_dtype != B.make_rows_desc(0, 1, self.dtype).dtype:
+            raise ValueError("the descriptor's gradients are not of %s, as the kept values are" % self.dtype)
         if desc.n * desc.h * desc.w != self.rows or desc.c != self.cols:
             raise ValueError("%d x %d values are kept, the layer has %d x %d" % (self.rows, self.cols, desc.n * desc.h * desc.w, desc.c))
         p = (desc.h + 2 * desc.pad_h - desc.r) // desc.stride_h + 1

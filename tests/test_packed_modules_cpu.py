@@ -249,3 +249,16 @@ def test_plans_asked_for_by_several_threads():
         return all(workspace(size) == want[size] for size in order)
     with ThreadPoolExecutor(8) as pool:
         assert all(pool.map(work, range(8)))
+
+
+def test_descriptors_of_another_type_are_refused(calls):
+    """The kernels read dy as what the descriptor says: bf16 gradients under an fp32 descriptor are half as long as what is read."""
+    for dtype, other in ((torch.bfloat16, torch.float32), (torch.float32, torch.bfloat16)):
+        packed, dy, dw = PackedActivation(4, 16, dtype, "e4m3", "cpu"), torch.zeros(4, 8, dtype=dtype), torch.zeros(8, 16)
+        desc = {t: B.make_desc(ConvLayer("linear", 4, 16, 1, 1, 8, 1, 1), t, dy_layout=B.DY_NPQK) for t in (dtype, other)}
+        with pytest.raises(ValueError, match="descriptor"):
+            packed.filter_gradient(dy, dw, desc[other])
+        assert not calls
+        packed.filter_gradient(dy, dw, desc[dtype])
+        assert calls.pop()[0] == "gaconv_dw_from_packed"
+        calls.clear()
