@@ -174,6 +174,8 @@ def make_desc(layer: ConvLayer, dtype: torch.dtype, *, x_layout=X_NHWC, dw_layou
     d.n, d.c, d.h, d.w, d.k, d.r, d.s = layer.n, layer.c, layer.h, layer.w, layer.k, layer.r, layer.s
     d.stride_h = d.stride_w = layer.stride
     d.pad_h = d.pad_w = layer.pad
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("layers are bf16 or fp32, not %s" % dtype)
     d.in_dtype = BF16 if dtype == torch.bfloat16 else F32
     d.x_layout, d.dy_layout, d.dw_layout = x_layout, dy_layout, dw_layout
     d.math, d.algo, d.topk, d.sm_budget = math, algo, topk, sm_budget

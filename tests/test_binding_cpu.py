@@ -7,6 +7,8 @@ import torch
 
 from paper_1908_05460_b200 import binding as B
 from paper_1908_05460_b200 import build as build_mod
+from paper_1908_05460_b200.autograd import GAConv2d
+from paper_1908_05460_b200.layers import config1_layer
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -48,3 +50,12 @@ def test_a_forked_process_hears_it_from_torch(monkeypatch):
         assert f.read() == b"torch"
     os.waitpid(pid, 0)
     assert B._cuda_runs          # the parent's own is left alone
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64, torch.int8, torch.float8_e4m3fn])
+def test_layers_of_other_types_are_refused(dtype):
+    """They were fp32 to the library, which reads four bytes an element."""
+    with pytest.raises(TypeError):
+        B.make_desc(config1_layer(), dtype)
+    with pytest.raises(TypeError):
+        GAConv2d(4, 8, 3, device="cpu").filter_gradient(torch.zeros(2, 4, 5, 5).to(dtype), torch.zeros(2, 8, 3, 3).to(dtype))
