@@ -91,7 +91,7 @@ class GAConv2d(torch.nn.Module):
         return _Conv2dFilterGrad.apply(x.contiguous(memory_format=torch.channels_last), self.weight, self)
 
     def _desc(self, x, dy_layout=B.DY_NKPQ):
-        key = (x.shape, x.dtype, dy_layout)
+        key = (x.shape, x.dtype, x.device, dy_layout)
         found = self._desc_cache.get(key)
         if found is None:
             n, c, h, w = x.shape

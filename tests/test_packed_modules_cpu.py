@@ -262,3 +262,11 @@ def test_descriptors_of_another_type_are_refused(calls):
         packed.filter_gradient(dy, dw, desc[dtype])
         assert calls.pop()[0] == "gaconv_dw_from_packed"
         calls.clear()
+
+
+def test_a_layer_moved_to_another_device_takes_a_workspace_there(calls):
+    layer = GAConv2d(4, 8, 3, 1, 1, device="cpu")
+    x = torch.zeros(2, 4, 5, 5)
+    here, there = layer._desc(x), layer._desc(x.to("meta"))
+    assert here is layer._desc(x) and here is not there
+    assert [ws.device.type for _, ws in layer._desc_cache.values()] == ["cpu", "meta"]
