@@ -220,7 +220,7 @@ typedef struct gaconv_rows_desc {
     int32_t  dtype;                    /* gaconv_dtype_t of the plain tensors                             */
     int32_t  format;                   /* gaconv_act_format_t of codes                                    */
     int64_t  x_stride, r_stride, s_stride, y_stride;   /* elements from a row to the next of x, residual, sum, y and of their gradients; 0: cols.
-                                          Multiples of 16 bytes are read fastest                          */
+                                          At most 2^40, and rows times a stride at most 2^60.  Multiples of 16 bytes are read fastest */
     float    eps;                      /* norm: added to the mean square, at least 0                      */
 } gaconv_rows_desc_t;
 

@@ -8,6 +8,7 @@ import torch
 
 import act8_ref as R
 from paper_1908_05460_b200 import binding as B
+from test_gpu_rmsnorm import Grad
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -53,3 +54,12 @@ def test_an_infinite_rstd_stays_in_its_row(dtype):
     B.gaconv_rmsnorm_backward(dy, None, s, w, rstd, dx, dw, d, B.rmsnorm_workspace(d))
     assert (dw == float("inf")).all()
     assert torch.isfinite(dx[0]).all() and torch.isfinite(dx[64:]).all()
+
+
+@pytest.mark.parametrize("cols", [8200, 8203])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_many_rows_beyond_the_registers(cols, dtype):
+    """Ranges of forty rows, and one that is shorter."""
+    g = Grad(2533, cols, dtype)
+    g.run()
+    g.check()
