@@ -98,7 +98,8 @@ class GAConv2d(torch.nn.Module):
             k = self.weight.shape[0]
             layer = ConvLayer("gaconv2d", n, c, h, w, k, self.kernel_size, self.kernel_size, self.stride, self.padding)
             d = B.make_desc(layer, x.dtype, x_layout=B.X_NHWC, dw_layout=B.DW_KCRS, alpha=1.0, dy_layout=dy_layout)
-            found = self._desc_cache[key] = (d, B.attach_workspace(d, methods=(B.METHOD_EXACT, B.METHOD_TOP1), device=x.device))
+            with torch.cuda.device(x.device):
+                found = self._desc_cache[key] = (d, B.attach_workspace(d, methods=(B.METHOD_EXACT, B.METHOD_TOP1), device=x.device))
         return found[0]
 
     @staticmethod
@@ -127,16 +128,18 @@ class GAConv2d(torch.nn.Module):
     def filter_gradient(self, x, dy):
         """dW [K,C,R,S] (the weight's dtype) of this layer for activations x and output gradient dy."""
         B.load()
+        check_devices(activations=x, gradient=dy, weight=self.weight)
         x = _on_boundary(x.contiguous(memory_format=torch.channels_last), torch.channels_last)        # NHWC memory under an NCHW-shaped tensor
         if dy.dtype != x.dtype:
             dy = dy.to(x.dtype)
         dy, dy_layout = self._dy_in_place(dy)
         dw = torch.empty(self.weight.shape, dtype=torch.float32, device=x.device)
         d = self._desc(x, dy_layout)
-        if self.schedule is None:
-            B.gaconv_dw_exact(x, dy, dw, d)
-        else:
-            self.schedule.run_layer(self.layer_index, self.step, x, dy, dw, d)
+        with torch.cuda.device(x.device):
+            if self.schedule is None:
+                B.gaconv_dw_exact(x, dy, dw, d)
+            else:
+                self.schedule.run_layer(self.layer_index, self.step, x, dy, dw, d)
         return dw.to(self.weight.dtype)
 
 

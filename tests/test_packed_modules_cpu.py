@@ -270,3 +270,25 @@ def test_a_layer_moved_to_another_device_takes_a_workspace_there(calls):
     here, there = layer._desc(x), layer._desc(x.to("meta"))
     assert here is layer._desc(x) and here is not there
     assert [ws.device.type for _, ws in layer._desc_cache.values()] == ["cpu", "meta"]
+
+
+def test_convolutions_off_the_current_device(calls, monkeypatch):
+    """The library's calls go to the current device, so that the tensors' one is made current around them; tensors of several are refused."""
+    current, at = [], []
+
+    @contextlib.contextmanager
+    def device(d):
+        current.append(d)
+        yield
+        current.pop()
+    monkeypatch.setattr(torch.cuda, "device", device)
+    for name in ("gaconv_dw_exact", "gaconv_workspace_init"):
+        monkeypatch.setattr(B, name, lambda *a, name=name, **k: at.append((name, list(current))))
+    layer = GAConv2d(4, 8, 3, 1, 1, device="cpu")
+    x, dy = torch.zeros(2, 4, 5, 5), torch.zeros(2, 8, 5, 5)
+    layer.filter_gradient(x, dy)
+    assert [name for name, _ in at] == ["gaconv_workspace_init", "gaconv_dw_exact"] and all(devices == [x.device] for _, devices in at)
+    for bad in ((x.to("meta"), dy), (x, dy.to("meta"))):
+        with pytest.raises(ValueError, match="several devices"):
+            layer.filter_gradient(*bad)
+    assert len(at) == 2
