@@ -129,6 +129,10 @@ class GAConv2d(torch.nn.Module):
         """dW [K,C,R,S] (the weight's dtype) of this layer for activations x and output gradient dy."""
         B.load()
         check_devices(activations=x, gradient=dy, weight=self.weight)
+        k, c, r, _ = self.weight.shape
+        out = [(size + 2 * self.padding - r) // self.stride + 1 for size in x.shape[2:]]
+        if x.dim() != 4 or x.shape[1] != c or dy.shape != (x.shape[0], k, *out):          # (the kernels go by x's shape alone)
+            raise ValueError("activations %s and a gradient %s of a layer of %s" % (tuple(x.shape), tuple(dy.shape), tuple(self.weight.shape)))
         x = _on_boundary(x.contiguous(memory_format=torch.channels_last), torch.channels_last)        # NHWC memory under an NCHW-shaped tensor
         if dy.dtype != x.dtype:
             dy = dy.to(x.dtype)

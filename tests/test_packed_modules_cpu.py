@@ -292,3 +292,16 @@ def test_convolutions_off_the_current_device(calls, monkeypatch):
         with pytest.raises(ValueError, match="several devices"):
             layer.filter_gradient(*bad)
     assert len(at) == 2
+
+
+def test_gradients_of_another_layer_are_refused(calls):
+    """A gradient that is smaller than the activations' shape says was read past its end."""
+    layer = GAConv2d(4, 8, 3, 2, 1, device="cpu")
+    x, dy = torch.zeros(2, 4, 7, 6), torch.zeros(2, 8, 4, 3)
+    layer.filter_gradient(x, dy)
+    assert calls.pop()[0] == "gaconv_dw_exact"
+    calls.clear()
+    for bad in ((x, dy[:1]), (x, dy[:, :7]), (x, dy[:, :, :3]), (x, dy[0]), (x[:, :3], dy), (x[0], dy), (torch.zeros(3, 4, 7, 6), dy), (torch.zeros(2, 4, 9, 6), dy)):
+        with pytest.raises(ValueError):
+            layer.filter_gradient(*bad)
+    assert not calls
